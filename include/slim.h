@@ -349,6 +349,59 @@ slim_status_t slim_linear_fwd_noalloc(const void* X, int b, const uint8_t* vals,
 size_t slim_noalloc_scratch_needed(int b, int d_out, int d_in, int r);
 
 /*
+ * 8-bit operands: the layers that a compressed model keeps out of the 4-bit 2:4 form, and what feeds a layer of either kind.
+ * (Inputs in 8-bit floating point, E4M3 or E5M2: App. "Input Quantization"; the scales here are one for 128 columns rather than one a
+ * tensor, so that a column with large values costs its neighbours no precision.)
+ *
+ * A matrix of values v is held as codes in an 8-bit floating-point format and binary32 scales; an element stands for code * scale of
+ * its group.  A group is 128 consecutive columns of a row (activations; [rows][ceil(columns / 128)] scales) or a block of 128 rows x 128
+ * columns (weights; [ceil(rows / 128)][ceil(columns / 128)]); the last groups of rows and columns may be smaller.  With top = 448 (E4M3)
+ * or 57344 (E5M2) and a = the largest |v| of the group,
+ *     scale = max(a / top, 2^-126),   inv = 1 / scale,   code = the 8-bit number nearest to clamp(v * inv, -top, top), ties to even,
+ * every step rounded to binary32, divisions correctly: codes and scales are reproducible bit for bit.  A group of zeros has scale
+ * 2^-126.  A NaN in a group makes its scale and all its codes NaN; an infinity makes the scale infinite, infinite elements NaN codes and
+ * the others 0 (so every product with the group is NaN).
+ *
+ * Shapes: rows >= 1; columns a multiple of 16 (else SLIM_ERR_UNSUPPORTED_SHAPE), at least 16.  All pointers are DEVICE pointers, 16-byte aligned; those
+ * of scales may be 4-byte aligned (rows of a larger batch).  Nothing here needs a workspace or keeps state between calls.
+ */
+typedef enum { SLIM_FP8_E4M3 = 0, SLIM_FP8_E5M2 = 1 } slim_fp8_t;
+typedef enum { SLIM_TYPE_BF16 = 0, SLIM_TYPE_F32 = 1 } slim_type_t;
+
+/*
+ * The residual's addition and the root-mean-square norm, in one pass, before a layer (activations X of Sec. 2 Eq. 1):
+ *     h = x + residual,   y = h / sqrt(mean over the row of h^2 + eps) * gamma
+ *   X [b, d] bf16; residual [b, d] bf16 or NULL (h = x); gamma [d] bf16; eps > 0, finite;
+ *   H [b, d] bf16 (out, may be NULL): h, the residual of the next step; it may be X or residual itself;
+ *   Y [b, d] bf16 (out): y, the input of slim_linear_fwd and its like.
+ * Everything is computed in binary32, from the unrounded h; H and Y are rounded once.  (A row whose sum of squares passes 3.4e38 comes out as zeros.)
+ * d <= 32768 (else SLIM_ERR_UNSUPPORTED_SHAPE).  Y must not overlap an input.
+ */
+slim_status_t slim_rmsnorm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, void* H, void* Y, void* cuda_stream);
+
+/* The same with y as 8-bit codes [b, d] and scales [b, ceil(d / 128)] (out), the input of slim_linear_fwd_fp8: y itself is quantised, in binary32. */
+slim_status_t slim_rmsnorm_fp8(const void* X, const void* residual, const void* gamma, float eps, int b, int d, slim_fp8_t format, void* H,
+                               void* codes, float* scales, void* cuda_stream);
+
+/* Activations X [b, d] bf16 that come from no norm (the input of an output or down projection) -> codes [b, d], scales [b, ceil(d / 128)]. */
+slim_status_t slim_quant_fp8(const void* X, int b, int d, slim_fp8_t format, void* codes, float* scales, void* cuda_stream);
+
+/* A weight W [d_out, d_in], bf16 or binary32 (`type`) -> codes [d_out, d_in], scales [ceil(d_out / 128), ceil(d_in / 128)], once per layer. */
+slim_status_t slim_pack_fp8(const void* W, slim_type_t type, int d_out, int d_in, slim_fp8_t format, void* codes, float* scales, void* cuda_stream);
+
+/*
+ * The forward of a layer whose weight is held in 8 bits (Sec. 2 Eq. 1):
+ *     Y[m][n] = sum over groups g of  Xs[m][g] * Ws[n / 128][g] * (sum over the columns k of g of Xq[m][k] Wq[n][k])
+ * Inner sums are made by the tensor cores, which accumulate in binary32; a group's sum is scaled and added to the others in binary32;
+ * Y [b, d_out] bf16 is rounded once (nearest even).  Bit-identical from run to run.  The product of the two scales of a group must be a
+ * finite binary32 number.
+ *   Xq [b, d_in] codes, Xs [b, ceil(d_in / 128)], Wq [d_out, d_in] codes, Ws [ceil(d_out / 128), ceil(d_in / 128)]; the formats may differ.
+ * Shape rules: b >= 1, d_in % 16 == 0, d_out >= 1 (any).
+ */
+slim_status_t slim_linear_fwd_fp8(const void* Xq, const float* Xs, slim_fp8_t x_format, int b, const void* Wq, const float* Ws, slim_fp8_t w_format,
+                                  int d_out, int d_in, void* Y, uint32_t* status_dev, void* cuda_stream);
+
+/*
  * The kernel family slim_linear_fwd would pick for this problem.  Asked for by name it runs the same kernel, except that
  * SLIM_KERNEL_PREFILL by name keeps to one CTA per tile in more cases (slim_last_token_tile tells which ran).
  */

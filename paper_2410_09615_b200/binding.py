@@ -52,6 +52,11 @@ SIGNATURES = {
     "slim_unpack_adapter": (_I, [_P, _P, _I, _I, _P, _P]),
     "slim_workspace_bytes_q": (_SZ, [_I, _I, _I, _I]),
     "slim_linear_fwd_q": (_I, [_P, _I, _P, _P, _F, _P, _P, _P, _P, _I, _I, _I, _P, _P, _SZ, _P, _P]),
+    "slim_rmsnorm": (_I, [_P, _P, _P, _F, _I, _I, _P, _P, _P]),
+    "slim_rmsnorm_fp8": (_I, [_P, _P, _P, _F, _I, _I, _I, _P, _P, _P, _P]),
+    "slim_quant_fp8": (_I, [_P, _I, _I, _I, _P, _P, _P]),
+    "slim_pack_fp8": (_I, [_P, _I, _I, _I, _I, _P, _P, _P]),
+    "slim_linear_fwd_fp8": (_I, [_P, _P, _I, _I, _P, _P, _I, _I, _I, _P, _P, _P]),
     "slim_select_kernel": (_I, [_I, _I, _I, _I]),
     "slim_decode_layout_hint": (_I, [_I, _I, _I, _I]),
     "slim_last_launch_count": (_I, []),
@@ -98,7 +103,8 @@ def native():
         spec.loader.exec_module(m)
         m.bind(SlimError, *[ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value for name in
                             ("slim_linear_fwd_ex", "slim_linear_fwd_tiled", "slim_linear_fwd_q", "slim_tiled_bytes", "slim_strerror",
-                             "slim_pack", "slim_quant", "slim_quant_workspace_bytes", "slim_mask_top2", "slim_pack_adapter")])
+                             "slim_pack", "slim_quant", "slim_quant_workspace_bytes", "slim_mask_top2", "slim_pack_adapter", "slim_rmsnorm", "slim_rmsnorm_fp8", "slim_quant_fp8",
+                             "slim_pack_fp8", "slim_linear_fwd_fp8")])
         _native = m
     return _native
 
@@ -322,3 +328,29 @@ def slim_quant(W: torch.Tensor, status=None):
 def slim_mask_top2(codes: torch.Tensor, xbar=None, status=None) -> torch.Tensor:
     """2:4 mask (uint8, like codes) of int8 codes; xbar: float32 [d_in] average input magnitudes, or None."""
     return (_native or native()).mask_top2(codes, xbar, status)
+
+
+def slim_rmsnorm(X: torch.Tensor, gamma: torch.Tensor, eps: float, residual=None, H=None, Y=None):
+    """Residual's addition and root-mean-square norm: (Y, H), both bf16 like X.  H = X + residual is the next step's residual: a given
+    tensor (which may be X or residual), else a new one, or None without a residual."""
+    return (_native or native()).rmsnorm(X, gamma, eps, residual, H, Y)
+
+
+def slim_rmsnorm_fp8(X: torch.Tensor, gamma: torch.Tensor, eps: float, residual=None, H=None, dtype=torch.float8_e4m3fn):
+    """The same with an 8-bit output: (codes like X, scales float32 [b, ceil(d / 128)], H).  ``dtype``: torch.float8_e4m3fn or float8_e5m2."""
+    return (_native or native()).rmsnorm_fp8(X, gamma, eps, residual, H, dtype)
+
+
+def slim_quant_fp8(X: torch.Tensor, dtype=torch.float8_e4m3fn):
+    """bf16 activations [b, d] -> (codes, scales float32 [b, ceil(d / 128)])."""
+    return (_native or native()).quant_fp8(X, dtype)
+
+
+def slim_pack_fp8(W: torch.Tensor, dtype=torch.float8_e4m3fn):
+    """bf16 or float32 weight [d_out, d_in] -> (codes, scales float32 [ceil(d_out / 128), ceil(d_in / 128)])."""
+    return (_native or native()).pack_fp8(W, dtype)
+
+
+def slim_linear_fwd_fp8(Xq: torch.Tensor, Xs: torch.Tensor, Wq: torch.Tensor, Ws: torch.Tensor, Y=None, status=None) -> torch.Tensor:
+    """Y = X W^T on 8-bit operands: codes and scales of slim_quant_fp8 or slim_rmsnorm_fp8, and of slim_pack_fp8.  Returns Y (bf16 [b, d_out])."""
+    return (_native or native()).linear_fwd_fp8(Xq, Xs, Wq, Ws, Y, status)

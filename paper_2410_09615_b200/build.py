@@ -10,7 +10,7 @@ INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libslim.so")
 NATIVE = os.path.join(HERE, "_slim_native.so")
 SOURCES = ["api.cu", "pack.cu", "repack.cu", "fwd_simple.cu", "fwd_small.cu", "fwd_prefill.cu",
-           "fwd_noalloc.cu", "adapter_q.cu", "quant_search.cu", "mask.cu"]
+           "fwd_noalloc.cu", "adapter_q.cu", "quant_search.cu", "mask.cu", "quant_fp8.cu", "fwd_fp8.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "--use_fast_math"]
 

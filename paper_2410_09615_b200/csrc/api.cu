@@ -389,6 +389,65 @@ slim_status_t slim_linear_fwd_host(const void* X_host, int b, const uint8_t* val
     return cudaStreamSynchronize(stream) == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
 }
 
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static bool is_fp8(int format) { return format == SLIM_FP8_E4M3 || format == SLIM_FP8_E5M2; }
+
+static slim_status_t check_norm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, const void* H) {
+    if (!X || !gamma || b < 1 || d < 1 || !(eps > 0.f) || !std::isfinite(eps)) return SLIM_ERR_INVALID_ARG;
+    if (d % 16 != 0 || d > 32768) return SLIM_ERR_UNSUPPORTED_SHAPE;
+    return aligned16(X) && aligned16(residual) && aligned16(gamma) && aligned16(H) ? SLIM_OK : SLIM_ERR_INVALID_ARG;
+}
+
+slim_status_t slim_rmsnorm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, void* H, void* Y, void* cuda_stream)
+{
+    reset_launch_count();
+    const slim_status_t st = check_norm(X, residual, gamma, eps, b, d, H);
+    if (!Y || !aligned16(Y) || Y == X || Y == residual || Y == gamma || Y == H) return SLIM_ERR_INVALID_ARG;
+    if (st != SLIM_OK) return st;
+    return launch_rmsnorm(X, residual, gamma, eps, b, d, H, Y, 0, nullptr, nullptr, (cudaStream_t)cuda_stream);
+}
+
+slim_status_t slim_rmsnorm_fp8(const void* X, const void* residual, const void* gamma, float eps, int b, int d, slim_fp8_t format, void* H,
+                               void* codes, float* scales, void* cuda_stream)
+{
+    reset_launch_count();
+    const slim_status_t st = check_norm(X, residual, gamma, eps, b, d, H);
+    if (!codes || !scales || !aligned16(codes) || !aligned4(scales) || !is_fp8(format)) return SLIM_ERR_INVALID_ARG;
+    if (st != SLIM_OK) return st;
+    return launch_rmsnorm(X, residual, gamma, eps, b, d, H, nullptr, format, codes, scales, (cudaStream_t)cuda_stream);
+}
+
+slim_status_t slim_quant_fp8(const void* X, int b, int d, slim_fp8_t format, void* codes, float* scales, void* cuda_stream)
+{
+    reset_launch_count();
+    if (!X || !codes || !scales || b < 1 || d < 1 || !is_fp8(format)) return SLIM_ERR_INVALID_ARG;
+    if (d % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(X) || !aligned16(codes) || !aligned4(scales)) return SLIM_ERR_INVALID_ARG;
+    return launch_quant_fp8(X, b, d, format, codes, scales, (cudaStream_t)cuda_stream);
+}
+
+slim_status_t slim_pack_fp8(const void* W, slim_type_t type, int d_out, int d_in, slim_fp8_t format, void* codes, float* scales, void* cuda_stream)
+{
+    reset_launch_count();
+    if (!W || !codes || !scales || d_out < 1 || d_in < 1 || !is_fp8(format) || (type != SLIM_TYPE_BF16 && type != SLIM_TYPE_F32)) return SLIM_ERR_INVALID_ARG;
+    if (d_in % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(W) || !aligned16(codes) || !aligned4(scales)) return SLIM_ERR_INVALID_ARG;
+    return launch_pack_fp8(W, type, d_out, d_in, format, codes, scales, (cudaStream_t)cuda_stream);
+}
+
+slim_status_t slim_linear_fwd_fp8(const void* Xq, const float* Xs, slim_fp8_t x_format, int b, const void* Wq, const float* Ws, slim_fp8_t w_format,
+                                  int d_out, int d_in, void* Y, uint32_t* status_dev, void* cuda_stream)
+{
+    reset_launch_count();
+    if (!Xq || !Xs || !Wq || !Ws || !Y || b < 1 || d_out < 1 || d_in < 1 || !is_fp8(x_format) || !is_fp8(w_format)) return SLIM_ERR_INVALID_ARG;
+    if (d_in % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(Xq) || !aligned16(Wq) || !aligned16(Y) || !aligned4(Xs) || !aligned4(Ws) || !aligned4(status_dev)) return SLIM_ERR_INVALID_ARG;
+    slim_status_t err;
+    if (!device_info(&err)) return err;
+    return launch_fp8(static_cast<const uint8_t*>(Xq), Xs, x_format, b, static_cast<const uint8_t*>(Wq), Ws, w_format, d_out, d_in,
+                      static_cast<__nv_bfloat16*>(Y), status_dev, (cudaStream_t)cuda_stream);
+}
+
 int slim_last_launch_count(void) { return t_launches; }
 
 int slim_last_token_tile(void) { return t_token_tile; }

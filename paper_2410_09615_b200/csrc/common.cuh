@@ -129,6 +129,14 @@ size_t quant_workspace_bytes(int d_out, int d_in);
 slim_status_t launch_quant(const float* W, int d_out, int d_in, int8_t* codes, float* scale_alpha, void* ws,
                            uint32_t* status_dev, cudaStream_t st);
 
+// 8-bit operands (formats and types as in slim.h).
+slim_status_t launch_rmsnorm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, void* H, void* Y,
+                             int format, void* codes, float* scales, cudaStream_t st);
+slim_status_t launch_quant_fp8(const void* X, int b, int d, int format, void* codes, float* scales, cudaStream_t st);
+slim_status_t launch_pack_fp8(const void* W, int type, int d_out, int d_in, int format, void* codes, float* scales, cudaStream_t st);
+slim_status_t launch_fp8(const uint8_t* Xq, const float* Xs, int x_format, int b, const uint8_t* Wq, const float* Ws, int w_format, int d_out, int d_in,
+                         __nv_bfloat16* Y, uint32_t* status_dev, cudaStream_t st);
+
 bool prefill_supports(int b, int d_out, int d_in, int r);
 size_t prefill_workspace_bytes(int b, int d_out, int d_in, int r);
 slim_status_t launch_prefill(const __nv_bfloat16* X, int b, const uint8_t* vals, const uint8_t* meta,

@@ -2,10 +2,12 @@
 // the call into libslim, without interpreted code in between.  A small-batch call takes the GPU about as long as
 // one launch takes the host, so the path from the interpreter to the launch is part of its time: through ctypes and
 // per-argument Python checks a call took the host 22-23 us, this way 4-8 (three to four of them the launch).
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime.h>
 #include <algorithm>
@@ -26,6 +28,11 @@ using QuantFn = int (*)(const float*, int, int, int8_t*, float*, void*, size_t, 
 using QuantBytesFn = size_t (*)(int, int);
 using MaskFn = int (*)(const int8_t*, const float*, int, int, uint8_t*, uint32_t*, void*);
 using AdapterFn = int (*)(const void*, int, int, uint8_t*, void*, void*);
+using NormFn = int (*)(const void*, const void*, const void*, float, int, int, void*, void*, void*);
+using Norm8Fn = int (*)(const void*, const void*, const void*, float, int, int, int, void*, void*, float*, void*);
+using Quant8Fn = int (*)(const void*, int, int, int, void*, float*, void*);
+using Pack8Fn = int (*)(const void*, int, int, int, int, void*, float*, void*);
+using Fwd8Fn = int (*)(const void*, const float*, int, int, const void*, const float*, int, int, int, void*, uint32_t*, void*);
 using TextFn = const char* (*)(int);
 
 FwdFn g_fwd = nullptr;
@@ -37,6 +44,11 @@ QuantFn g_quant = nullptr;
 QuantBytesFn g_quant_bytes = nullptr;
 MaskFn g_mask = nullptr;
 AdapterFn g_pack_adapter = nullptr;
+NormFn g_norm = nullptr;
+Norm8Fn g_norm8 = nullptr;
+Quant8Fn g_quant8 = nullptr;
+Pack8Fn g_pack8 = nullptr;
+Fwd8Fn g_fwd8 = nullptr;
 TextFn g_text = nullptr;
 PyObject* g_error = nullptr;            // SlimError(code, where, text)
 
@@ -336,11 +348,191 @@ PyObject* quant(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- 8-bit operands.  These calls run on the device of their tensors, whichever is current, on its current stream.
+// A tensor's 8-bit format (slim_fp8_t), or -1.
+int fp8_format(at::ScalarType t) { return t == at::kFloat8_e4m3fn ? 0 : t == at::kFloat8_e5m2 ? 1 : -1; }
+
+bool fp8_type(PyObject* o, at::ScalarType* type) {
+    if (THPDtype_Check(o)) {
+        *type = reinterpret_cast<THPDtype*>(o)->scalar_type;
+        if (fp8_format(*type) >= 0) return true;
+    }
+    PyErr_SetString(PyExc_TypeError, "dtype: expected torch.float8_e4m3fn or torch.float8_e5m2");
+    return false;
+}
+
+const at::Tensor* fp8_tensor(PyObject* o, const char* name) {
+    if (THPVariable_Check(o)) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (t.is_cuda() && fp8_format(t.scalar_type()) >= 0 && t.is_contiguous()) return &t;
+    }
+    PyErr_Format(PyExc_TypeError, "%s: expected a contiguous CUDA tensor of torch.float8_e4m3fn or torch.float8_e5m2", name);
+    return nullptr;
+}
+
+// A matrix of this shape on this device.
+bool is_matrix(const at::Tensor& t, int64_t rows, int64_t cols, const at::Tensor& beside, const char* name) {
+    if (t.dim() == 2 && t.size(0) == rows && t.size(1) == cols && t.device() == beside.device()) return true;
+    PyErr_Format(PyExc_ValueError, "%s: expected shape (%lld, %lld) on the device of the other tensors", name, (long long)rows, (long long)cols);
+    return false;
+}
+
+// Sizes that the library takes as int.
+bool fits(std::initializer_list<int64_t> sizes) {
+    for (int64_t n : sizes)
+        if (n > 0x7FFFFFFF) { PyErr_SetString(PyExc_ValueError, "a size passes 2^31 - 1"); return false; }
+    return true;
+}
+
+int64_t groups_of(int64_t n) { return (n + 127) / 128; }
+
+// The optional status word: an int32 on the same device.
+bool status_word(PyObject* o, const at::Tensor& beside, void** p) {
+    *p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = device_tensor(o, at::kInt, "status", "torch.int32");
+    if (!t) return false;
+    if (t->numel() < 1 || t->device() != beside.device()) { PyErr_SetString(PyExc_ValueError, "status: expected a word on the device of the other tensors"); return false; }
+    *p = t->data_ptr();
+    return true;
+}
+
+// A matrix that the call fills: the given one, checked, or a new one.
+bool filled(PyObject* given, at::Tensor* made, int64_t rows, int64_t cols, const at::Tensor& like, const char* name) {
+    if (given == Py_None) { *made = fresh({rows, cols}, at::kBFloat16, like); return true; }
+    const at::Tensor* t = bf16_tensor(given, name);
+    if (!t || !is_matrix(*t, rows, cols, like, name)) return false;
+    *made = *t;
+    return true;
+}
+
+PyObject* tensor_or_none(at::Tensor t) {
+    if (t.defined()) return THPVariable_Wrap(std::move(t));
+    Py_RETURN_NONE;
+}
+
+struct NormArgs { const at::Tensor *X, *gamma, *residual; at::Tensor H; float eps; int64_t b, d; };
+
+// (X, gamma, eps, residual, H) of both norms
+bool norm_args(PyObject* const* a, NormArgs* n) {
+    n->X = bf16_tensor(a[0], "X");
+    if (!n->X || !rank2(n->X, "X")) return false;
+    n->gamma = bf16_tensor(a[1], "gamma");
+    if (!n->gamma) return false;
+    n->eps = (float)PyFloat_AsDouble(a[2]);
+    if (PyErr_Occurred()) return false;
+    n->b = n->X->size(0); n->d = n->X->size(1);
+    if (!fits({n->b, n->d})) return false;
+    if (n->gamma->dim() != 1 || n->gamma->size(0) != n->d || n->gamma->device() != n->X->device()) {
+        PyErr_SetString(PyExc_ValueError, "gamma: expected a vector of X's columns on X's device");
+        return false;
+    }
+    n->residual = nullptr;
+    if (a[3] != Py_None) {
+        n->residual = bf16_tensor(a[3], "residual");
+        if (!n->residual || !is_matrix(*n->residual, n->b, n->d, *n->X, "residual")) return false;
+    }
+    return (a[4] == Py_None && !n->residual) || filled(a[4], &n->H, n->b, n->d, *n->X, "H");
+}
+
+// rmsnorm(X, gamma, eps, residual, H, Y) -> (Y, H)
+PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!bound(n, 6)) return nullptr;
+    NormArgs g;
+    at::Tensor Y;
+    if (!norm_args(a, &g)) return nullptr;
+    c10::cuda::CUDAGuard guard(g.X->device());
+    if (!filled(a[5], &Y, g.b, g.d, *g.X, "Y")) return nullptr;
+    const int rc = unlocked(g_norm, g.X->data_ptr(), g.residual ? g.residual->data_ptr() : nullptr, g.gamma->data_ptr(), g.eps, (int)g.b, (int)g.d,
+                            g.H.defined() ? g.H.data_ptr() : nullptr, Y.data_ptr(), c10::cuda::getCurrentCUDAStream().stream());
+    if (rc != 0) return finish(rc, nullptr, "slim_rmsnorm");
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(Y)), tensor_or_none(std::move(g.H)));
+    END_HANDLE_TH_ERRORS
+}
+
+// rmsnorm_fp8(X, gamma, eps, residual, H, dtype) -> (codes, scales, H)
+PyObject* rmsnorm_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!bound(n, 6)) return nullptr;
+    NormArgs g;
+    at::ScalarType type;
+    if (!fp8_type(a[5], &type) || !norm_args(a, &g)) return nullptr;
+    c10::cuda::CUDAGuard guard(g.X->device());
+    at::Tensor codes = fresh({g.b, g.d}, type, *g.X), scales = fresh({g.b, groups_of(g.d)}, at::kFloat, *g.X);
+    const int rc = unlocked(g_norm8, g.X->data_ptr(), g.residual ? g.residual->data_ptr() : nullptr, g.gamma->data_ptr(), g.eps, (int)g.b, (int)g.d,
+                            fp8_format(type), g.H.defined() ? g.H.data_ptr() : nullptr, codes.data_ptr(), (float*)scales.data_ptr(),
+                            c10::cuda::getCurrentCUDAStream().stream());
+    if (rc != 0) return finish(rc, nullptr, "slim_rmsnorm_fp8");
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(codes)), THPVariable_Wrap(std::move(scales)), tensor_or_none(std::move(g.H)));
+    END_HANDLE_TH_ERRORS
+}
+
+// quant_fp8(X, dtype) -> (codes, scales)
+PyObject* quant_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!bound(n, 2)) return nullptr;
+    at::ScalarType type;
+    const at::Tensor* X = bf16_tensor(a[0], "X");
+    if (!X || !rank2(X, "X") || !fp8_type(a[1], &type)) return nullptr;
+    const int64_t b = X->size(0), d = X->size(1);
+    if (!fits({b, d})) return nullptr;
+    c10::cuda::CUDAGuard guard(X->device());
+    at::Tensor codes = fresh({b, d}, type, *X), scales = fresh({b, groups_of(d)}, at::kFloat, *X);
+    const int rc = unlocked(g_quant8, X->data_ptr(), (int)b, (int)d, fp8_format(type), codes.data_ptr(), (float*)scales.data_ptr(),
+                            c10::cuda::getCurrentCUDAStream().stream());
+    if (rc != 0) return finish(rc, nullptr, "slim_quant_fp8");
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(codes)), THPVariable_Wrap(std::move(scales)));
+    END_HANDLE_TH_ERRORS
+}
+
+// pack_fp8(W, dtype) -> (codes, scales)
+PyObject* pack_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!bound(n, 2)) return nullptr;
+    at::ScalarType type;
+    const bool f32 = THPVariable_Check(a[0]) && THPVariable_Unpack(a[0]).scalar_type() == at::kFloat;
+    const at::Tensor* W = f32 ? device_tensor(a[0], at::kFloat, "W", "torch.float32") : device_tensor(a[0], at::kBFloat16, "W", "torch.bfloat16 or torch.float32");
+    if (!W || !rank2(W, "W") || !fp8_type(a[1], &type)) return nullptr;
+    const int64_t d_out = W->size(0), d_in = W->size(1);
+    if (!fits({d_out, d_in})) return nullptr;
+    c10::cuda::CUDAGuard guard(W->device());
+    at::Tensor codes = fresh({d_out, d_in}, type, *W), scales = fresh({groups_of(d_out), groups_of(d_in)}, at::kFloat, *W);
+    const int rc = unlocked(g_pack8, W->data_ptr(), f32 ? 1 : 0, (int)d_out, (int)d_in, fp8_format(type), codes.data_ptr(), (float*)scales.data_ptr(),
+                            c10::cuda::getCurrentCUDAStream().stream());
+    if (rc != 0) return finish(rc, nullptr, "slim_pack_fp8");
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(codes)), THPVariable_Wrap(std::move(scales)));
+    END_HANDLE_TH_ERRORS
+}
+
+// linear_fwd_fp8(Xq, Xs, Wq, Ws, Y, status) -> Y
+PyObject* linear_fwd_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!bound(n, 6)) return nullptr;
+    const at::Tensor *Xq = fp8_tensor(a[0], "Xq"), *Xs = Xq ? device_tensor(a[1], at::kFloat, "Xs", "torch.float32") : nullptr;
+    const at::Tensor *Wq = Xs ? fp8_tensor(a[2], "Wq") : nullptr, *Ws = Wq ? device_tensor(a[3], at::kFloat, "Ws", "torch.float32") : nullptr;
+    if (!Ws || !rank2(Xq, "Xq") || !rank2(Wq, "Wq")) return nullptr;
+    const int64_t b = Xq->size(0), d_in = Xq->size(1), d_out = Wq->size(0);
+    if (!fits({b, d_in, d_out}) || !is_matrix(*Wq, d_out, d_in, *Xq, "Wq") || !is_matrix(*Xs, b, groups_of(d_in), *Xq, "Xs") ||
+        !is_matrix(*Ws, groups_of(d_out), groups_of(d_in), *Xq, "Ws"))
+        return nullptr;
+    c10::cuda::CUDAGuard guard(Xq->device());
+    at::Tensor Y;
+    void* status;
+    if (!status_word(a[5], *Xq, &status) || !filled(a[4], &Y, b, d_out, *Xq, "Y")) return nullptr;
+    const int rc = unlocked(g_fwd8, Xq->data_ptr(), (const float*)Xs->data_ptr(), fp8_format(Xq->scalar_type()), (int)b, Wq->data_ptr(),
+                            (const float*)Ws->data_ptr(), fp8_format(Wq->scalar_type()), (int)d_out, (int)d_in, Y.data_ptr(), (uint32_t*)status,
+                            c10::cuda::getCurrentCUDAStream().stream());
+    if (rc != 0) return finish(rc, nullptr, "slim_linear_fwd_fp8");
+    return THPVariable_Wrap(std::move(Y));
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(SlimError, addresses of the functions in the loaded libslim)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject* err;
-    unsigned long long f, t, q, by, tx, pk, qu, qb, mk, pa;
-    if (!PyArg_ParseTuple(args, "OKKKKKKKKKK", &err, &f, &t, &q, &by, &tx, &pk, &qu, &qb, &mk, &pa)) return nullptr;
+    unsigned long long f, t, q, by, tx, pk, qu, qb, mk, pa, rn, r8, q8, p8, f8;
+    if (!PyArg_ParseTuple(args, "OKKKKKKKKKKKKKKK", &err, &f, &t, &q, &by, &tx, &pk, &qu, &qb, &mk, &pa, &rn, &r8, &q8, &p8, &f8)) return nullptr;
     Py_INCREF(err);
     Py_XDECREF(g_error);
     g_error = err;
@@ -348,6 +540,8 @@ PyObject* bind(PyObject*, PyObject* args) {
     g_tiled_bytes = reinterpret_cast<BytesFn>(by); g_text = reinterpret_cast<TextFn>(tx);
     g_pack = reinterpret_cast<PackFn>(pk); g_quant = reinterpret_cast<QuantFn>(qu); g_quant_bytes = reinterpret_cast<QuantBytesFn>(qb);
     g_mask = reinterpret_cast<MaskFn>(mk); g_pack_adapter = reinterpret_cast<AdapterFn>(pa);
+    g_norm = reinterpret_cast<NormFn>(rn); g_norm8 = reinterpret_cast<Norm8Fn>(r8); g_quant8 = reinterpret_cast<Quant8Fn>(q8);
+    g_pack8 = reinterpret_cast<Pack8Fn>(p8); g_fwd8 = reinterpret_cast<Fwd8Fn>(f8);
     Py_RETURN_NONE;
 }
 
@@ -360,6 +554,11 @@ PyMethodDef methods[] = {
     {"mask_top2", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(mask_top2)), METH_FASTCALL, nullptr},
     {"pack_adapter", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(pack_adapter)), METH_FASTCALL, nullptr},
     {"quant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(quant)), METH_FASTCALL, nullptr},
+    {"rmsnorm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(rmsnorm)), METH_FASTCALL, nullptr},
+    {"rmsnorm_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(rmsnorm_fp8)), METH_FASTCALL, nullptr},
+    {"quant_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(quant_fp8)), METH_FASTCALL, nullptr},
+    {"pack_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(pack_fp8)), METH_FASTCALL, nullptr},
+    {"linear_fwd_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(linear_fwd_fp8)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_slim_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
