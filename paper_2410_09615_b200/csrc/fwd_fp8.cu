@@ -31,6 +31,14 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint32_t a_lo, uint32_t 
         "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, p;\n\t}"
         :: "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
 }
+__device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a, b, %3, p;\n\t}"
+        :: "r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
+}
 
 // 16 rows x 8 A columns of a buffer: four values an eight columns.  The wait names the registers, so nothing that uses them is moved ahead of it.
 template <int A> struct Frag { float v[A][4]; };
@@ -57,9 +65,26 @@ __device__ __forceinline__ void tmem_wait(Frag<A>& f, Frag<A>& g) {
     }
 }
 
-// acc += v * s, for two neighbouring tokens.
+// 16 columns of this thread's row of a buffer; the wait as above.
+__device__ __forceinline__ void tmem_ld_row(uint32_t taddr, float (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+                   "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_row(float (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
+                   "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]) :: "memory");
+}
+
+// acc += v * s, for two neighbouring columns.
 __device__ __forceinline__ void fma2(unsigned long long& acc, float v0, float v1, unsigned long long s) {
     asm("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}" : "+l"(acc) : "f"(v0), "f"(v1), "l"(s));
+}
+__device__ __forceinline__ unsigned long long pair_of(float a, float b) {
+    unsigned long long v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
 }
 __device__ __forceinline__ float2 halves(unsigned long long v) {
     float2 f;
@@ -69,6 +94,11 @@ __device__ __forceinline__ float2 halves(unsigned long long v) {
 __device__ __forceinline__ unsigned long long lds64(uint32_t addr) {
     unsigned long long v;
     asm volatile("ld.shared.b64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float lds32(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
 __device__ __forceinline__ void sts32(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" :: "r"(addr), "f"(v) : "memory"); }
@@ -109,6 +139,47 @@ __device__ __forceinline__ void store_frag(__nv_bfloat16* Y, int d_out, int row,
         if (r0 + 1 < d_out) to[1] = two_lo.y;
         if (r0 + 8 < d_out) to[8] = two_hi.x;
         if (r0 + 9 < d_out) to[9] = two_hi.y;
+    }
+}
+
+// A warp's walk over `count` groups from `first` on: the scales of a tile's tokens (32 a lane and step, EACH steps at most) times the
+// block's, into the slots of a ring, of which `before` uses came before.  AHEAD groups' loads are under way while the ones before are handed over.
+template <int EACH, int AHEAD, int SLOTS>
+__device__ __forceinline__ void bring_scales(const float* Xs, const float* ws, int groups, int first, int count, int n0, int b, int each, uint32_t ring, uint32_t slot_bytes,
+                                             uint64_t* full, uint64_t* empty, int before, int lane, volatile uint32_t* abort_flag, bool& ok)
+{
+    float v[AHEAD][EACH], w[AHEAD];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const bool in = i0 + j < count;
+            w[j] = in ? ws[first + i0 + j] : 0.f;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const int n = n0 + lane + 32 * e;
+                v[j][e] = in && e < each && n < b ? Xs[(size_t)n * groups + first + i0 + j] : 0.f;
+            }
+        }
+    };
+    load(0);
+    for (int i0 = 0; i0 < count; i0 += AHEAD) {
+        float s[AHEAD][EACH];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) s[j][e] = v[j][e] * w[j];
+        load(i0 + AHEAD);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int g = before + i0 + j, slot = g % SLOTS;
+            if (i0 + j >= count) break;
+            if (g >= SLOTS) ok = mbar_wait(&empty[slot], ((g / SLOTS) & 1) ^ 1, abort_flag) && ok;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e)
+                if (e < each && (uint32_t)(lane + 32 * e) * 4 < slot_bytes) sts32(ring + slot * slot_bytes + (lane + 32 * e) * 4, s[j][e]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&full[slot]);
+        }
     }
 }
 
@@ -220,40 +291,8 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
         }
     } else if (warp == 6) {
         // ============================ scales: of the tokens times the block's ============================
-        constexpr int kAhead = 4, kEach = (N + 31) / 32;
-        const float* ws = p.Ws + (size_t)tile * p.groups + g0;
-        float v[kAhead][kEach], w[kAhead];
-        auto load = [&](int i0) {
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                w[j] = i0 + j < n_groups ? ws[i0 + j] : 0.f;
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) {
-                    const int n = lane + 32 * e;
-                    v[j][e] = n < N && n0 + n < p.b && i0 + j < n_groups ? p.Xs[(size_t)(n0 + n) * p.groups + g0 + i0 + j] : 0.f;
-                }
-            }
-        };
-        load(0);
-        for (int i0 = 0; i0 < n_groups; i0 += kAhead) {
-            float s[kAhead][kEach];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j)
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) s[j][e] = v[j][e] * w[j];
-            load(i0 + kAhead);
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int i = i0 + j, slot = i % kSlots;
-                if (i >= n_groups) break;
-                if (i >= kSlots) ok = mbar_wait(&sc_empty[slot], ((i / kSlots) & 1) ^ 1, abort_flag) && ok;
-#pragma unroll
-                for (int e = 0; e < kEach; ++e)
-                    if (lane + 32 * e < N) sts32(s32(smem + Cfg::kOffScales) + (slot * N + lane + 32 * e) * 4, s[j][e]);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sc_full[slot]);
-            }
-        }
+        bring_scales<(N + 31) / 32, 4, kSlots>(p.Xs, p.Ws + (size_t)tile * p.groups, p.groups, g0, n_groups, n0, p.b, (N + 31) / 32, s32(smem + Cfg::kOffScales), N * 4,
+                                               sc_full, sc_empty, 0, lane, abort_flag, ok);
     } else {
         // ============================ accumulation ============================
         constexpr int kA = Cfg::kChunk / 8, kChunks = N / Cfg::kChunk;
@@ -335,12 +374,280 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
     }
 }
 
+// ---------------------------------------------------------------- pairs of CTAs: many tokens
+// Persistent clusters of two CTAs walk tiles of 256 tokens x up to 256 rows (n, a multiple of 64) with cta_group::2 MMAs that the even CTA
+// issues: each CTA loads its own 128 tokens and half of the tile's rows, and accumulates its 128 tokens.  All rings run on across
+// tiles, so the next tile's groups are multiplied while this tile is stored.
+// Tokens are the MMA's rows here: a thread has one token, so the product of a group's scales is one number for each 128 rows of the
+// weight, and the buffer is read with tcgen05.ld 32x32b, 64 words a cycle and quarter of the SM (16x256b: 16, so that a buffer of
+// 128 x 256 took as long to read as to multiply).
+// Warps: 0-7 accumulate (32 tokens x half of the rows each), 8 requests tiles by TMA, 9 issues MMAs, 10 brings the scales.
+struct PairCfg8 {
+    static constexpr int kWarps = 8, kThreads = (kWarps + 4) * 32;
+    static constexpr int kRegs = 224, kOtherRegs = 56;                      // 2 x 224 + 56 = 3 x 168, what the three warpgroups are launched with
+    static constexpr int kStages = 5, kStage = 32768, kOffW = kF8Group * kF8Group;     // the tokens' tile, then the weight's
+    static constexpr int kScales = 2 * kF8Group * 4;                                   // of a group: 128 tokens x two blocks
+    static constexpr int kOffOut = kStages * kStage, kOutSlot = 4096;                  // a warp's 32 tokens x 64 rows on their way out
+    static constexpr int kOffScales = kOffOut + kWarps * kOutSlot, kOffBars = kOffScales + 8 * kScales;
+    static constexpr size_t kSmem = 1024 + kOffBars + 256;
+    static_assert(kSmem <= 227 * 1024, "shared memory");
+};
+
+struct alignas(128) Fp8PairParams {
+    __nv_bfloat16* Y;
+    const float* Xs; const float* Ws;
+    uint32_t* status;
+    int b, d_out, groups;
+    uint32_t idesc;
+    int row_tiles, token_tiles, token_group;     // tiles of a group of token tiles follow each other, token tiles first
+    int by_tma;             // rows of Y are a multiple of 16 bytes
+};
+
+template <int N>
+__global__ void __launch_bounds__(PairCfg8::kThreads, 1)
+fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmY)
+{
+    using namespace f8;
+    using Cfg = PairCfg8;
+    constexpr int kStages = Cfg::kStages, kBufferCols = N <= 128 ? 128 : 256, kBuffers = 512 / kBufferCols, kSlots = 2 * kBuffers;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kOffBars);      // [kStages] even CTA: both CTAs' tiles landed
+    uint64_t* empty = full + kStages;                // [kStages] the MMAs that read the stage are complete
+    uint64_t* acc_full = empty + kStages;            // [kBuffers] a group's MMAs are complete, its scales and the next one's are there
+    uint64_t* acc_empty = acc_full + kBuffers;       // [kBuffers] even CTA: the warps of both CTAs have read the buffer
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + kBuffers);
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int pairs = gridDim.x >> 1, tiles = p.row_tiles * p.token_tiles;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+        for (int i = 0; i < kBuffers; ++i) { mbar_init(&acc_full[i], 2); mbar_init(&acc_empty[i], 2 * Cfg::kWarps); }
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8 && elect_one()) { prefetch_map(&tmX); prefetch_map(&tmW); prefetch_map(&tmY); }
+    cluster_sync_all();                              // both CTAs' barriers exist before anything crosses
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(s32(tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(tmem_slot), 0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");            // what the grid before wrote is read through TMA
+    bool ok = true;
+    // A tile's first token in this CTA and its first row.
+    struct Tile { int m0, n0; };
+    auto tile_of = [&](int t) {
+        const int per = p.token_group * p.row_tiles, group = t / per, in = t - group * per;
+        const int here = min(p.token_group, p.token_tiles - group * p.token_group), rt = in / here;
+        return Tile{(2 * (group * p.token_group + in - rt * here) + (int)rank) * kF8Group, rt * N};
+    };
+
+    // (the roles stand inside the branches that set the registers: behind them the compiler would have to reckon with the smaller number)
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(Cfg::kRegs));
+        // ============================ accumulation, then a tile's end ============================
+        constexpr int half = N / 2, kChunks = half / 16;
+        const int side = warp >> 2, quarter = warp & 3;
+        const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + side * half;
+        const uint32_t out = s32(smem + Cfg::kOffOut) + warp * Cfg::kOutSlot, give = peer_addr(acc_empty, 0);
+        const uint32_t scales = s32(smem + Cfg::kOffScales) + side * 512 + quarter * 128 + lane * 4;
+        int g = 0;
+        float next = 0.f;
+        for (int t = blockIdx.x >> 1; t < tiles; t += pairs) {
+            const Tile ti = tile_of(t);
+            const int row0 = ti.n0 + side * half, tok0 = ti.m0 + quarter * 32;
+            unsigned long long acc[half / 2] = {};           // neighbouring rows of the weight
+            for (int i = 0; i < p.groups; ++i, ++g) {
+                const int buf = g % kBuffers;
+                const uint32_t ta = t0 + buf * kBufferCols;
+                ok = mbar_wait(&acc_full[buf], (g / kBuffers) & 1, abort_flag) && ok;
+                fence_after_sync();
+                float f[2][16];
+                tmem_ld_row(ta, f[0]);
+                // (a group's scales are there a group before: the read takes a hundred cycles)
+                if (g == 0) next = lds32(scales);
+                const unsigned long long s = pair_of(next, next);
+                next = lds32(scales + ((g + 1) % kSlots) * Cfg::kScales);
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    tmem_wait_row(f[c & 1]);
+                    if (c + 1 < kChunks) tmem_ld_row(ta + (c + 1) * 16, f[(c + 1) & 1]);
+                    else {
+                        fence_before_sync();
+                        __syncwarp();
+                        if (elect_one()) mbar_arrive_remote(give + buf * 8);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) fma2(acc[c * 8 + k], f[c & 1][2 * k], f[c & 1][2 * k + 1], s);
+                }
+            }
+            // 64 rows of the weight at a time into the warp's place in shared memory, [token][64 rows] bf16, 128-byte swizzle, and out from there
+#pragma unroll
+            for (int c = 0; c < half / 64; ++c) {
+                if (row0 + c * 64 >= p.d_out || tok0 >= p.b) break;
+                const uint32_t place = out;
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 v = halves(acc[c * 32 + k * 4 + e]);
+                        const __nv_bfloat162 two = __floats2bfloat162_rn(v.x, v.y);
+                        w[e] = *reinterpret_cast<const uint32_t*>(&two);
+                    }
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(place + lane * 128 + ((uint32_t)(k ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                }
+                if (p.by_tma) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
+                                     :: "l"(&tmY), "r"(row0 + c * 64), "r"(tok0), "r"(place) : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                } else {
+                    __syncwarp();
+                    for (int k = 0; k < 32; ++k) {                  // a token; two rows a lane
+                        if (tok0 + k >= p.b) break;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int r = lane + 32 * e;
+                            uint16_t v;
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(place + k * 128 + ((((uint32_t)r >> 3) ^ ((uint32_t)k & 7)) << 4) + (r & 7) * 2) : "memory");
+                            if (row0 + c * 64 + r < p.d_out) reinterpret_cast<uint16_t*>(p.Y)[(size_t)(tok0 + k) * p.d_out + row0 + c * 64 + r] = v;
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(Cfg::kOtherRegs));
+        if (warp == 8) {
+            // ============================ tiles ============================
+            constexpr int half = N / 2;
+            int g = 0;
+            for (int t = blockIdx.x >> 1; t < tiles; t += pairs) {
+                const Tile ti = tile_of(t);
+                for (int i = 0; i < p.groups; ++i, ++g) {
+                    const int st = g % kStages;
+                    if (g >= kStages) ok = mbar_wait(&empty[st], ((g / kStages) & 1) ^ 1, abort_flag) && ok;
+                    unsigned char* at = smem + st * Cfg::kStage;
+                    if (elect_one()) {
+                        // (the odd CTA's bytes are counted on the even one's barrier too, which cannot end the phase before it has announced all)
+                        if (rank == 0) mbar_expect_tx(&full[st], (uint32_t)(2 * (kF8Group + half) * kF8Group));
+                        const uint32_t bar = peer_addr(&full[st], 0);
+                        tma_tile_pair(at, &tmX, i * kF8Group, ti.m0, bar);
+                        tma_tile_pair(at + Cfg::kOffW, &tmW, i * kF8Group, ti.n0 + (int)rank * half, bar);
+                    }
+                }
+            }
+        } else if (warp == 9) {
+            // ============================ MMA issue: a warp of the even CTA ============================
+            if (rank == 0) {
+                int g = 0;
+                bool there = false;                          // the coming stage was found full by an early question
+                const uint32_t first = desc_lo(s32(smem));
+                for (int t = blockIdx.x >> 1; t < tiles; t += pairs) {
+                    for (int i = 0; i < p.groups; ++i, ++g) {
+                        const int st = g % kStages, buf = g % kBuffers, use = g / kBuffers;
+                        if (!there) ok = mbar_wait(&full[st], (g / kStages) & 1, abort_flag) && ok;
+                        if (use > 0) ok = mbar_wait(&acc_empty[buf], (use & 1) ^ 1, abort_flag) && ok;
+                        fence_after_sync();
+                        const uint32_t x = first + (uint32_t)st * (Cfg::kStage >> 4), w = x + (Cfg::kOffW >> 4), d = tmem_base + (uint32_t)(buf * kBufferCols);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) mma_f8_pair(d, x + 2 * j, w + 2 * j, p.idesc, j > 0 ? 1u : 0u);
+                            mma_commit2(&acc_full[buf]);
+                            mma_commit2(&empty[st]);
+                        }
+                        there = __all_sync(0xffffffffu, mbar_test(&full[(g + 1) % kStages], ((g + 1) / kStages) & 1, false));
+                    }
+                }
+            }
+        } else if (warp == 10) {
+            // ============================ scales: of the tokens times the blocks' ============================
+            // They go into a ring a group ahead: this warp's arrival for a group says that the next one's are there too.  A slot was last read
+            // for the group 2 kBuffers before, by warps that have given its buffer back since: that buffer's next MMAs are complete when this
+            // warp has seen acc_full.
+            const int blocks = ceil_div(p.d_out, kF8Group);
+            int g = 0;
+            auto free = [&](int of) {                        // waits until the arrival for group `of` is the next on its buffer's barrier
+                const int buf = of % kBuffers, use = of / kBuffers;
+                if (use > 0) ok = mbar_wait(&acc_full[buf], (use & 1) ^ 1, abort_flag) && ok;
+            };
+            for (int t = blockIdx.x >> 1; t < tiles; t += pairs) {
+                const Tile ti = tile_of(t);
+                constexpr int kAhead = 2;
+                const float* xs[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) xs[e] = p.Xs + (size_t)min(ti.m0 + lane + 32 * e, p.b - 1) * p.groups;
+                const float* w0 = p.Ws + (size_t)min(ti.n0 / kF8Group, blocks - 1) * p.groups;
+                const float* w1 = p.Ws + (size_t)min((ti.n0 + N / 2) / kF8Group, blocks - 1) * p.groups;
+                float v[kAhead][4], w[kAhead][2];
+                auto load = [&](int i0) {
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j) {
+                        const int i = min(i0 + j, p.groups - 1);
+                        w[j][0] = w0[i]; w[j][1] = w1[i];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[j][e] = xs[e][i];
+                    }
+                };
+                load(0);
+                for (int i0 = 0; i0 < p.groups; i0 += kAhead) {
+                    float s[kAhead][2][4];
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) s[j][e >> 2][e & 3] = v[j][e & 3] * w[j][e >> 2];
+                    load(i0 + kAhead);
+#pragma unroll
+                    for (int j = 0; j < kAhead; ++j, ++g) {
+                        if (i0 + j >= p.groups) break;
+                        if (g > 0) free(g - 1);
+                        const uint32_t at = s32(smem + Cfg::kOffScales) + (g % kSlots) * Cfg::kScales + lane * 4;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sts32(at + e * 128, s[j][e >> 2][e & 3]);
+                        __syncwarp();
+                        if (g > 0 && lane == 0) mbar_arrive(&acc_full[(g - 1) % kBuffers]);
+                    }
+                }
+            }
+            free(g - 1);
+            if (lane == 0) mbar_arrive(&acc_full[(g - 1) % kBuffers]);
+        }
+    }
+
+    if (!ok && lane == 0) flag_error(p.status, SLIM_ERR_TIMEOUT);
+    fence_before_sync();
+    __syncthreads();
+    cluster_sync_all();                              // neither CTA leaves while the other may still use its shared memory
+    if (warp == 9) {
+        fence_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(512) : "memory");
+    }
+}
+
 // ---------------------------------------------------------------- host side
 // 8-bit rows of d_in bytes: boxes of 128 columns x box_rows rows, 128-byte swizzle.
 static bool f8_map(CUtensorMap* map, const void* base, int d_in, int rows, int box_rows) {
     return pf_map(map, base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, (uint64_t)d_in, (uint64_t)rows, kF8Group, box_rows, 128);
 }
 
+static std::atomic<int> g_f8_pairs[64];            // pairs resident at once
 static std::atomic<bool> g_f8_attr_set[64];        // attributes set once per device (setting them twice is harmless)
 
 template <int N>
@@ -366,6 +673,36 @@ static slim_status_t launch_small8(Fp8Params p, const void* Xq, int x_format, co
     return e == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
 }
 
+template <int N>
+static slim_status_t launch_pair8(const Fp8Params& q, const void* Xq, int x_format, const void* Wq, int w_format, int d_in, int pairs, cudaStream_t st) {
+    using Cfg = PairCfg8;
+    Fp8PairParams p = {};
+    p.Y = q.Y; p.Xs = q.Xs; p.Ws = q.Ws; p.status = q.status; p.b = q.b; p.d_out = q.d_out; p.groups = q.groups;
+    p.token_tiles = ceil_div(q.b, 2 * kF8Group);
+    p.row_tiles = ceil_div(q.d_out, N);
+    p.token_group = p.token_tiles < 8 ? p.token_tiles : 8;
+    p.idesc = f8::idesc_f8(2 * kF8Group, N, x_format, w_format);
+    p.by_tma = q.d_out % 8 == 0;
+    CUtensorMap tmW, tmX, tmY;
+    if (!f8_map(&tmW, Wq, d_in, q.d_out, N / 2) || !f8_map(&tmX, Xq, d_in, q.b, kF8Group)) return SLIM_ERR_CUDA;
+    tmY = tmX;                                   // not used where rows of Y are no multiple of 16 bytes
+    if (p.by_tma && !pf_map(&tmY, q.Y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (uint64_t)q.d_out, (uint64_t)q.b, 64, 32, 128)) return SLIM_ERR_CUDA;
+    const long long tiles = (long long)p.row_tiles * p.token_tiles;
+    if (tiles > 0x7FFFFFFFll - 256) return SLIM_ERR_INVALID_ARG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))); cfg.blockDim = dim3(Cfg::kThreads); cfg.dynamicSmemBytes = Cfg::kSmem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fp8_pair_kernel<N>, p, tmX, tmW, tmY);
+    count_launch(1);
+    note_token_tile(256);
+    return e == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
+}
+
 slim_status_t launch_fp8(const uint8_t* Xq, const float* Xs, int x_format, int b, const uint8_t* Wq, const float* Ws, int w_format, int d_out, int d_in,
                          __nv_bfloat16* Y, uint32_t* status_dev, cudaStream_t st)
 {
@@ -379,12 +716,29 @@ slim_status_t launch_fp8(const uint8_t* Xq, const float* Xs, int x_format, int b
         if (cudaFuncSetAttribute(fp8_small_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SmallCfg8<16>::kSmem) != cudaSuccess ||
             cudaFuncSetAttribute(fp8_small_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SmallCfg8<32>::kSmem) != cudaSuccess ||
             cudaFuncSetAttribute(fp8_small_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SmallCfg8<64>::kSmem) != cudaSuccess ||
+            cudaFuncSetAttribute(fp8_pair_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairCfg8::kSmem) != cudaSuccess ||
+            cudaFuncSetAttribute(fp8_pair_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairCfg8::kSmem) != cudaSuccess ||
             cudaFuncSetAttribute(fp8_small_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SmallCfg8<128>::kSmem) != cudaSuccess)
             return SLIM_ERR_CUDA;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(2); cfg.blockDim = dim3(PairCfg8::kThreads); cfg.dynamicSmemBytes = PairCfg8::kSmem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr; cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, fp8_pair_kernel<256>, &cfg) != cudaSuccess || n < 1) return SLIM_ERR_CUDA;
+        g_f8_pairs[dev].store(n < di->sm_count / 2 ? n : di->sm_count / 2, std::memory_order_relaxed);
         g_f8_attr_set[dev].store(true, std::memory_order_release);
     }
     Fp8Params p = {};
     p.Y = Y; p.Xs = Xs; p.Ws = Ws; p.status = status_dev; p.b = b; p.d_out = d_out; p.groups = ceil_div(d_in, kF8Group);
+    if (b > 128) {
+        const int pairs = g_f8_pairs[dev].load(std::memory_order_relaxed);
+        const long long t256 = (long long)ceil_div(b, 256) * ceil_div(d_out, 256), t128 = (long long)ceil_div(b, 256) * ceil_div(d_out, 128);
+        return (t256 + pairs - 1) / pairs * 4 <= (t128 + pairs - 1) / pairs * 3 ? launch_pair8<256>(p, Xq, x_format, Wq, w_format, d_in, pairs, st)
+                                                                              : launch_pair8<128>(p, Xq, x_format, Wq, w_format, d_in, pairs, st);
+    }
     return b <= 16   ? launch_small8<16>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st)
            : b <= 32 ? launch_small8<32>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st)
            : b <= 64 ? launch_small8<64>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st)
