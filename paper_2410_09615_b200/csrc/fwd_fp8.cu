@@ -10,7 +10,9 @@
 // c = 2 (lane % 4) and c + 1: four values, two pairs of tokens, so that a lane needs the scales of a quarter of the tokens (as pairs, the
 // operand of fma.f32x2) instead of all of them.
 #include <atomic>
+#include <mutex>
 #include "fp8.cuh"
+#include "fp8_plan.h"
 #include "tcgen05.cuh"
 
 namespace slim {
@@ -394,18 +396,23 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
 // weight, and the buffer is read with tcgen05.ld 32x32b, 64 words a cycle and quarter of the SM (16x256b: 16, so that a buffer of
 // 128 x 256 took as long to read as to multiply).
 // Warps: 0-7 accumulate (32 tokens x half of the rows each), 8 requests tiles by TMA, 9 issues MMAs, 10 brings the scales.
-struct PairCfg8 {
-    static constexpr int kWarps = 8, kThreads = (kWarps + 4) * 32;
-    static constexpr int kRegs = 216, kOtherRegs = 72;                      // 2 x 216 + 72 = 3 x 168, what the three warpgroups are launched with
-    static constexpr int kStages = 5, kStage = 32768, kOffW = kF8Group * kF8Group;     // the tokens' tile, then the weight's
-    static constexpr int kScales = 2 * kF8Group * 32, kScaleSlots = 2;                 // of eight groups: 128 tokens x two blocks
-    static constexpr int kOffOut = kStages * kStage, kOutSlot = 4096;                  // a warp's 32 tokens x 64 rows on their way out
-    static constexpr int kOffScales = kOffOut + kWarps * kOutSlot, kOffBars = kOffScales + kScaleSlots * kScales;
+// PAIR false: single CTAs on tiles of 128 tokens x N rows (32, 64 or 128), for layers whose pair tiles would leave most SMs without one; a warp
+// then accumulates all rows of its 32 tokens.
+template <int N, bool PAIR> struct TokCfg8 {
+    static constexpr int kWarps = PAIR ? 8 : 4, kThreads = (kWarps + 4) * 32;            // .. kWarps tiles, + 1 MMAs, + 2 scales
+    static constexpr int kRegs = 216, kOtherRegs = 72;                                  // pairs: 2 x 216 + 72 = 3 x 168, what the three warpgroups are launched with
+    static constexpr int kSides = PAIR ? 2 : 1, kCols = N / kSides;                     // columns of a warp
+    static constexpr int kRowsW = PAIR ? N / 2 : N;                                     // of the weight that a CTA loads
+    static constexpr int kOffW = kF8Group * kF8Group, kStage = kOffW + kRowsW * kF8Group, kStages = 163840 / kStage;
+    static constexpr int kBufferCols = N <= 128 ? 128 : 256, kBuffers = 512 / kBufferCols;
+    static constexpr int kScales = kSides * kF8Group * 32, kSlots = 2;                  // of eight groups: 128 tokens x the sides' blocks
+    static constexpr int kOutCols = kCols < 64 ? kCols : 64, kOutSlot = 32 * kOutCols * 2;      // a warp's 32 tokens x 64 (32) rows on their way out
+    static constexpr int kOffOut = kStages * kStage, kOffScales = kOffOut + kWarps * kOutSlot, kOffBars = kOffScales + kSlots * kScales;
     static constexpr size_t kSmem = 1024 + kOffBars + 256;
-    static_assert(kSmem <= 227 * 1024, "shared memory");
+    static_assert(kSmem <= 227 * 1024 && kStage % 1024 == 0 && (2 * kStages + 2 * kBuffers + 2 * kSlots) * 8 + 8 <= 256, "shared memory");
 };
 
-struct alignas(128) Fp8PairParams {
+struct alignas(128) Fp8TokensParams {
     __nv_bfloat16* Y;
     const float* Xs; const float* Ws;
     uint32_t* status;
@@ -415,13 +422,14 @@ struct alignas(128) Fp8PairParams {
     int by_tma;             // rows of Y are a multiple of 16 bytes
 };
 
-template <int N>
-__global__ void __launch_bounds__(PairCfg8::kThreads, 1)
-fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmY)
+template <int N, bool PAIR>
+__global__ void __launch_bounds__(TokCfg8<N, PAIR>::kThreads, 1)
+fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmY)
 {
     using namespace f8;
-    using Cfg = PairCfg8;
-    constexpr int kStages = Cfg::kStages, kBufferCols = N <= 128 ? 128 : 256, kBuffers = 512 / kBufferCols, kSlots = Cfg::kScaleSlots;
+    using Cfg = TokCfg8<N, PAIR>;
+    constexpr int kStages = Cfg::kStages, kBufferCols = Cfg::kBufferCols, kBuffers = Cfg::kBuffers, kSlots = Cfg::kSlots, kWarps = Cfg::kWarps, kSides = Cfg::kSides, kCols = Cfg::kCols;
+    constexpr int kCtas = PAIR ? 2 : 1;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kOffBars);      // [kStages] even CTA: both CTAs' tiles landed
@@ -434,21 +442,26 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
     volatile uint32_t* abort_flag = tmem_slot + 1;
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank();
-    const int pairs = gridDim.x >> 1, tiles = p.row_tiles * p.token_tiles;
+    const uint32_t rank = PAIR ? cluster_rank() : 0u;
+    const int units = gridDim.x / kCtas, first_tile = blockIdx.x / kCtas, tiles = p.row_tiles * p.token_tiles;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-        for (int i = 0; i < kBuffers; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 2 * Cfg::kWarps); }
-        for (int i = 0; i < kSlots; ++i) { mbar_init(&sc_full[i], 1); mbar_init(&sc_empty[i], Cfg::kWarps); }
+        for (int i = 0; i < kBuffers; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], kCtas * kWarps); }
+        for (int i = 0; i < kSlots; ++i) { mbar_init(&sc_full[i], 1); mbar_init(&sc_empty[i], kWarps); }
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8 && elect_one()) { prefetch_map(&tmX); prefetch_map(&tmW); prefetch_map(&tmY); }
-    cluster_sync_all();                              // both CTAs' barriers exist before anything crosses
-    if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(s32(tmem_slot)), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    if (warp == kWarps && elect_one()) { prefetch_map(&tmX); prefetch_map(&tmW); prefetch_map(&tmY); }
+    if (PAIR) cluster_sync_all();                    // both CTAs' barriers exist before anything crosses
+    if (warp == kWarps + 1) {
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(s32(tmem_slot)), "r"(512) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(s32(tmem_slot)), "r"(512) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     fence_before_sync();
     __syncthreads();
@@ -462,23 +475,23 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
     auto tile_of = [&](int t) {
         const int per = p.token_group * p.row_tiles, group = t / per, in = t - group * per;
         const int here = min(p.token_group, p.token_tiles - group * p.token_group), rt = in / here;
-        return Tile{(2 * (group * p.token_group + in - rt * here) + (int)rank) * kF8Group, rt * N};
+        return Tile{(kCtas * (group * p.token_group + in - rt * here) + (int)rank) * kF8Group, rt * N};
     };
 
     // (the roles stand inside the branches that set the registers: behind them the compiler would have to reckon with the smaller number)
-    if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(Cfg::kRegs));
+    if (warp < kWarps) {
+        if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(Cfg::kRegs));
         // ============================ accumulation, then a tile's end ============================
-        constexpr int half = N / 2, kChunks = half / 16;
+        constexpr int kChunks = kCols / 16;
         const int side = warp >> 2, quarter = warp & 3;
-        const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + side * half;
-        const uint32_t out = s32(smem + Cfg::kOffOut) + warp * Cfg::kOutSlot, give = peer_addr(acc_empty, 0);
-        const uint32_t scales = s32(smem + Cfg::kOffScales) + side * (Cfg::kScales / 2) + (quarter * 32 + lane) * 32;
+        const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + side * kCols;
+        const uint32_t out = s32(smem + Cfg::kOffOut) + warp * Cfg::kOutSlot, give = PAIR ? peer_addr(acc_empty, 0) : 0u;
+        const uint32_t scales = s32(smem + Cfg::kOffScales) + side * (Cfg::kScales / kSides) + (quarter * 32 + lane) * 32;
         int g = 0, eights = 0;
-        for (int t = blockIdx.x >> 1; t < tiles; t += pairs) {
+        for (int t = first_tile; t < tiles; t += units) {
             const Tile ti = tile_of(t);
-            const int row0 = ti.n0 + side * half, tok0 = ti.m0 + quarter * 32;
-            unsigned long long acc[half / 2] = {};           // neighbouring rows of the weight
+            const int row0 = ti.n0 + side * kCols, tok0 = ti.m0 + quarter * 32;
+            unsigned long long acc[kCols / 2] = {};           // neighbouring rows of the weight
             float4 s4 = make_float4(0.f, 0.f, 0.f, 0.f);     // this token's scales of the next groups, times the block's
 #pragma unroll 1
             for (int i = 0; i < p.groups; ++i, ++g) {
@@ -507,36 +520,40 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
                     else {
                         fence_before_sync();
                         __syncwarp();
-                        if (elect_one()) mbar_arrive_remote(give + buf * 8);
+                        if (elect_one()) { if (PAIR) mbar_arrive_remote(give + buf * 8); else mbar_arrive(&acc_empty[buf]); }
                     }
 #pragma unroll
                     for (int k = 0; k < 8; ++k) fma2(acc[c * 8 + k], f[c & 1][2 * k], f[c & 1][2 * k + 1], s);
                 }
             }
-            // 64 rows of the weight at a time into the warp's place in shared memory, [token][64 rows] bf16, 128-byte swizzle, and out from there
+            // 64 rows of the weight (32) at a time into the warp's place in shared memory, [token][64 rows] bf16, 128-byte (64-byte) swizzle,
+            // and out from there
+            constexpr int kOut = Cfg::kOutCols;
+            auto place_of = [&](int token, int chunk) {      // of eight rows
+                return out + token * (kOut * 2) + ((uint32_t)(chunk ^ (kOut == 64 ? token & 7 : (token >> 1) & 3)) << 4);
+            };
 #pragma unroll
-            for (int c = 0; c < half / 64; ++c) {
-                if (row0 + c * 64 >= p.d_out || tok0 >= p.b) break;
-                const uint32_t place = out;
+            for (int c = 0; c < kCols / kOut; ++c) {
+                if (row0 + c * kOut >= p.d_out || tok0 >= p.b) break;
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                 __syncwarp();
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < kOut / 8; ++k) {
                     uint32_t w[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float2 v = halves(acc[c * 32 + k * 4 + e]);
+                        const float2 v = halves(acc[c * (kOut / 2) + k * 4 + e]);
                         const __nv_bfloat162 two = __floats2bfloat162_rn(v.x, v.y);
                         w[e] = *reinterpret_cast<const uint32_t*>(&two);
                     }
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(place + lane * 128 + ((uint32_t)(k ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(place_of(lane, k)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
                 }
                 if (p.by_tma) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) {
                         asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];"
-                                     :: "l"(&tmY), "r"(row0 + c * 64), "r"(tok0), "r"(place) : "memory");
+                                     :: "l"(&tmY), "r"(row0 + c * kOut), "r"(tok0), "r"(out) : "memory");
                         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
                 } else {
@@ -544,11 +561,11 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
                     for (int k = 0; k < 32; ++k) {                  // a token; two rows a lane
                         if (tok0 + k >= p.b) break;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
+                        for (int e = 0; e < kOut / 32; ++e) {
                             const int r = lane + 32 * e;
                             uint16_t v;
-                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(place + k * 128 + ((((uint32_t)r >> 3) ^ ((uint32_t)k & 7)) << 4) + (r & 7) * 2) : "memory");
-                            if (row0 + c * 64 + r < p.d_out) reinterpret_cast<uint16_t*>(p.Y)[(size_t)(tok0 + k) * p.d_out + row0 + c * 64 + r] = v;
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(place_of(k, r >> 3) + (r & 7) * 2) : "memory");
+                            if (row0 + c * kOut + r < p.d_out) reinterpret_cast<uint16_t*>(p.Y)[(size_t)(tok0 + k) * p.d_out + row0 + c * kOut + r] = v;
                         }
                     }
                     __syncwarp();
@@ -557,12 +574,11 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(Cfg::kOtherRegs));
-        if (warp == 8) {
+        if (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(Cfg::kOtherRegs));
+        if (warp == kWarps) {
             // ============================ tiles ============================
-            constexpr int half = N / 2;
             int g = 0;
-            for (int t = blockIdx.x >> 1; t < tiles; t += pairs) {
+            for (int t = first_tile; t < tiles; t += units) {
                 const Tile ti = tile_of(t);
                 for (int i = 0; i < p.groups; ++i, ++g) {
                     const int st = g % kStages;
@@ -570,20 +586,25 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
                     unsigned char* at = smem + st * Cfg::kStage;
                     if (elect_one()) {
                         // (the odd CTA's bytes are counted on the even one's barrier too, which cannot end the phase before it has announced all)
-                        if (rank == 0) mbar_expect_tx(&full[st], (uint32_t)(2 * (kF8Group + half) * kF8Group));
-                        const uint32_t bar = peer_addr(&full[st], 0);
-                        tma_tile_pair(at, &tmX, i * kF8Group, ti.m0, bar);
-                        tma_tile_pair(at + Cfg::kOffW, &tmW, i * kF8Group, ti.n0 + (int)rank * half, bar);
+                        if (rank == 0) mbar_expect_tx(&full[st], (uint32_t)(kCtas * Cfg::kStage));
+                        if (PAIR) {
+                            const uint32_t bar = peer_addr(&full[st], 0);
+                            tma_tile_pair(at, &tmX, i * kF8Group, ti.m0, bar);
+                            tma_tile_pair(at + Cfg::kOffW, &tmW, i * kF8Group, ti.n0 + (int)rank * Cfg::kRowsW, bar);
+                        } else {
+                            tma_tile(at, &tmX, i * kF8Group, ti.m0, &full[st]);
+                            tma_tile(at + Cfg::kOffW, &tmW, i * kF8Group, ti.n0, &full[st]);
+                        }
                     }
                 }
             }
-        } else if (warp == 9) {
+        } else if (warp == kWarps + 1) {
             // ============================ MMA issue: a warp of the even CTA ============================
             if (rank == 0) {
                 int g = 0;
                 bool there = false;                          // the coming stage was found full by an early question
                 const uint32_t first = desc_lo(s32(smem));
-                for (int t = blockIdx.x >> 1; t < tiles; t += pairs) {
+                for (int t = first_tile; t < tiles; t += units) {
                     for (int i = 0; i < p.groups; ++i, ++g) {
                         const int st = g % kStages, buf = g % kBuffers, use = g / kBuffers;
                         if (!there) warp_wait(&full[st], (g / kStages) & 1, abort_flag);
@@ -592,28 +613,31 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
                         const uint32_t x = first + (uint32_t)st * (Cfg::kStage >> 4), w = x + (Cfg::kOffW >> 4), d = tmem_base + (uint32_t)(buf * kBufferCols);
                         if (elect_one()) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) mma_f8_pair(d, x + 2 * j, w + 2 * j, p.idesc, j > 0 ? 1u : 0u);
-                            mma_commit2(&acc_full[buf]);
-                            mma_commit2(&empty[st]);
+                            for (int j = 0; j < 4; ++j) {
+                                if (PAIR) mma_f8_pair(d, x + 2 * j, w + 2 * j, p.idesc, j > 0 ? 1u : 0u);
+                                else      mma_f8(d, x + 2 * j, w + 2 * j, p.idesc, j > 0 ? 1u : 0u);
+                            }
+                            if (PAIR) { mma_commit2(&acc_full[buf]); mma_commit2(&empty[st]); }
+                            else      { mma_commit(&acc_full[buf]); mma_commit(&empty[st]); }
                         }
                         there = __all_sync(0xffffffffu, mbar_test(&full[(g + 1) % kStages], ((g + 1) / kStages) & 1, false));
                     }
                 }
             }
-        } else if (warp == 10) {
+        } else if (warp == kWarps + 2) {
             // ============================ scales: of the tokens times the blocks' ============================
             // Eight groups at a time, [block][token][group]: a lane loads group lane % 8 of every fourth token, so that a load touches four
             // lines (a token a lane: 32, and the barriers and loads of the other warps waited behind them: 740 cycles a group instead of 690).
             const int blocks = ceil_div(p.d_out, kF8Group), k = lane & 7;
             int eights = 0;
-            for (int t = blockIdx.x >> 1; t < tiles; t += pairs) {
+            for (int t = first_tile; t < tiles; t += units) {
                 const Tile ti = tile_of(t);
                 const float* w0 = p.Ws + (size_t)min(ti.n0 / kF8Group, blocks - 1) * p.groups;
-                const float* w1 = p.Ws + (size_t)min((ti.n0 + N / 2) / kF8Group, blocks - 1) * p.groups;
+                const float* w1 = p.Ws + (size_t)min((ti.n0 + N / kSides) / kF8Group, blocks - 1) * p.groups;
                 const int tok0 = ti.m0 + (lane >> 3);
                 for (int i0 = 0; i0 < p.groups; i0 += 8, ++eights) {
                     const int slot = eights % kSlots, i = min(i0 + k, p.groups - 1);
-                    const float wa = w0[i], wb = w1[i];
+                    const float wa = w0[i], wb = PAIR ? w1[i] : 0.f;
                     const uint32_t at = s32(smem + Cfg::kOffScales) + slot * Cfg::kScales + lane * 4;
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
@@ -624,7 +648,7 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             sts32(at + (half * 16 + e) * 128, v[e] * wa);
-                            sts32(at + (half * 16 + e) * 128 + Cfg::kScales / 2, v[e] * wb);
+                            if (PAIR) sts32(at + (half * 16 + e) * 128 + Cfg::kScales / 2, v[e] * wb);
                         }
                     }
                     __syncwarp();
@@ -637,10 +661,11 @@ fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMap tmX, 
     fence_before_sync();
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) flag_error(p.status, SLIM_ERR_TIMEOUT);
-    cluster_sync_all();                              // neither CTA leaves while the other may still use its shared memory
-    if (warp == 9) {
+    if (PAIR) cluster_sync_all();                    // neither CTA leaves while the other may still use its shared memory
+    if (warp == kWarps + 1) {
         fence_after_sync();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(512) : "memory");
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(512) : "memory");
+        else      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(512) : "memory");
     }
 }
 
@@ -650,18 +675,65 @@ static bool f8_map(CUtensorMap* map, const void* base, int d_in, int rows, int b
     return pf_map(map, base, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, (uint64_t)d_in, (uint64_t)rows, kF8Group, box_rows, 128);
 }
 
-static std::atomic<int> g_f8_pairs[64];            // pairs resident at once
-static std::atomic<bool> g_f8_attr_set[64];        // attributes set once per device (setting them twice is harmless)
+// Attributes and what is resident at once, per device: set and found once (twice is harmless, both find the same).
+struct Fp8Device { int pairs; int clusters[4][4]; };
+static Fp8Device g_f8[64];
+static std::atomic<bool> g_f8_ready[64];
+
+// Clusters of a kernel that are resident at once (0: the launch would fail).
+template <typename K>
+static int resident_clusters(K kernel, int ctas, int threads, size_t smem) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    int n = 0;
+    return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess ? n : 0;
+}
+template <typename K>
+static bool large_smem(K kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess; }
 
 template <int N>
-static slim_status_t launch_small8(Fp8Params p, const void* Xq, int x_format, const void* Wq, int w_format, int d_in, int sm_count, cudaStream_t st) {
+static bool prepare_small8(int (&clusters)[4]) {
+    using Cfg = SmallCfg8<N>;
+    if (!large_smem(fp8_small_kernel<N>, Cfg::kSmem)) return false;
+    for (int i = 0; i < 4; ++i)
+        if ((clusters[i] = resident_clusters(fp8_small_kernel<N>, 1 << i, Cfg::kThreads, Cfg::kSmem)) < 1) return false;
+    return true;
+}
+template <int N, bool PAIR>
+static bool prepare_tokens8() { return large_smem(fp8_tokens_kernel<N, PAIR>, TokCfg8<N, PAIR>::kSmem); }
+
+static const Fp8Device* fp8_device(const DeviceInfo* di) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    if (!g_f8_ready[dev].load(std::memory_order_acquire)) {
+        static std::mutex m;
+        std::lock_guard<std::mutex> lock(m);
+        if (!g_f8_ready[dev].load(std::memory_order_relaxed)) {
+            Fp8Device& d = g_f8[dev];
+            if (!prepare_small8<16>(d.clusters[0]) || !prepare_small8<32>(d.clusters[1]) || !prepare_small8<64>(d.clusters[2]) || !prepare_small8<128>(d.clusters[3]) ||
+                !prepare_tokens8<32, false>() || !prepare_tokens8<64, false>() || !prepare_tokens8<128, false>() || !prepare_tokens8<128, true>() ||
+                !prepare_tokens8<256, true>())
+                return nullptr;
+            const int n = resident_clusters(fp8_tokens_kernel<256, true>, 2, TokCfg8<256, true>::kThreads, TokCfg8<256, true>::kSmem);
+            if (n < 1) return nullptr;
+            d.pairs = n < di->sm_count / 2 ? n : di->sm_count / 2;
+            g_f8_ready[dev].store(true, std::memory_order_release);
+        }
+    }
+    return &g_f8[dev];
+}
+
+template <int N>
+static slim_status_t launch_small8(Fp8Params p, const void* Xq, int x_format, const void* Wq, int w_format, int d_in, int ctas, cudaStream_t st) {
     using Cfg = SmallCfg8<N>;
     p.idesc = f8::idesc_f8(kF8Group, N, w_format, x_format);
     CUtensorMap tmW, tmX;
     if (!f8_map(&tmW, Wq, d_in, p.d_out, kF8Group) || !f8_map(&tmX, Xq, d_in, p.b, N)) return SLIM_ERR_CUDA;
     const int tiles = ceil_div(p.d_out, kF8Group), token_tiles = ceil_div(p.b, N);
-    int ctas = 8;
-    while (ctas > 1 && ((long long)tiles * token_tiles * ctas > (long long)sm_count * Cfg::kCtasPerSm || p.groups < 2 * ctas)) ctas /= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * ctas), (unsigned)token_tiles); cfg.blockDim = dim3(Cfg::kThreads); cfg.dynamicSmemBytes = Cfg::kSmem; cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -676,33 +748,34 @@ static slim_status_t launch_small8(Fp8Params p, const void* Xq, int x_format, co
     return e == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
 }
 
-template <int N>
-static slim_status_t launch_pair8(const Fp8Params& q, const void* Xq, int x_format, const void* Wq, int w_format, int d_in, int pairs, cudaStream_t st) {
-    using Cfg = PairCfg8;
-    Fp8PairParams p = {};
+template <int N, bool PAIR>
+static slim_status_t launch_tokens8(const Fp8Params& q, const void* Xq, int x_format, const void* Wq, int w_format, int d_in, int units, cudaStream_t st) {
+    using Cfg = TokCfg8<N, PAIR>;
+    constexpr int kCtas = PAIR ? 2 : 1;
+    Fp8TokensParams p = {};
     p.Y = q.Y; p.Xs = q.Xs; p.Ws = q.Ws; p.status = q.status; p.b = q.b; p.d_out = q.d_out; p.groups = q.groups;
-    p.token_tiles = ceil_div(q.b, 2 * kF8Group);
+    p.token_tiles = ceil_div(q.b, kCtas * kF8Group);
     p.row_tiles = ceil_div(q.d_out, N);
     p.token_group = p.token_tiles < 8 ? p.token_tiles : 8;
-    p.idesc = f8::idesc_f8(2 * kF8Group, N, x_format, w_format);
+    p.idesc = f8::idesc_f8(kCtas * kF8Group, N, x_format, w_format);
     p.by_tma = q.d_out % 8 == 0;
     CUtensorMap tmW, tmX, tmY;
-    if (!f8_map(&tmW, Wq, d_in, q.d_out, N / 2) || !f8_map(&tmX, Xq, d_in, q.b, kF8Group)) return SLIM_ERR_CUDA;
+    if (!f8_map(&tmW, Wq, d_in, q.d_out, Cfg::kRowsW) || !f8_map(&tmX, Xq, d_in, q.b, kF8Group)) return SLIM_ERR_CUDA;
     tmY = tmX;                                   // not used where rows of Y are no multiple of 16 bytes
-    if (p.by_tma && !pf_map(&tmY, q.Y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (uint64_t)q.d_out, (uint64_t)q.b, 64, 32, 128)) return SLIM_ERR_CUDA;
+    if (p.by_tma && !pf_map(&tmY, q.Y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (uint64_t)q.d_out, (uint64_t)q.b, Cfg::kOutCols, 32, Cfg::kOutCols * 2)) return SLIM_ERR_CUDA;
     const long long tiles = (long long)p.row_tiles * p.token_tiles;
     if (tiles > 0x7FFFFFFFll - 256) return SLIM_ERR_INVALID_ARG;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))); cfg.blockDim = dim3(Cfg::kThreads); cfg.dynamicSmemBytes = Cfg::kSmem; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(kCtas * (tiles < units ? tiles : units))); cfg.blockDim = dim3(Cfg::kThreads); cfg.dynamicSmemBytes = Cfg::kSmem; cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = 2;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, fp8_pair_kernel<N>, p, tmX, tmW, tmY);
+    cfg.attrs = attr + (PAIR ? 0 : 1); cfg.numAttrs = PAIR ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fp8_tokens_kernel<N, PAIR>, p, tmX, tmW, tmY);
     count_launch(1);
-    note_token_tile(256);
+    note_token_tile(kCtas * kF8Group);
     return e == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
 }
 
@@ -712,40 +785,23 @@ slim_status_t launch_fp8(const uint8_t* Xq, const float* Xs, int x_format, int b
     slim_status_t err;
     const DeviceInfo* di = device_info(&err);
     if (!di) return err;
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (dev < 0 || dev >= 64) return SLIM_ERR_CUDA;
-    if (!g_f8_attr_set[dev].load(std::memory_order_acquire)) {
-        if (cudaFuncSetAttribute(fp8_small_kernel<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SmallCfg8<16>::kSmem) != cudaSuccess ||
-            cudaFuncSetAttribute(fp8_small_kernel<32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SmallCfg8<32>::kSmem) != cudaSuccess ||
-            cudaFuncSetAttribute(fp8_small_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SmallCfg8<64>::kSmem) != cudaSuccess ||
-            cudaFuncSetAttribute(fp8_pair_kernel<256>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairCfg8::kSmem) != cudaSuccess ||
-            cudaFuncSetAttribute(fp8_pair_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairCfg8::kSmem) != cudaSuccess ||
-            cudaFuncSetAttribute(fp8_small_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SmallCfg8<128>::kSmem) != cudaSuccess)
-            return SLIM_ERR_CUDA;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(2); cfg.blockDim = dim3(PairCfg8::kThreads); cfg.dynamicSmemBytes = PairCfg8::kSmem;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr; cfg.numAttrs = 1;
-        int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, fp8_pair_kernel<256>, &cfg) != cudaSuccess || n < 1) return SLIM_ERR_CUDA;
-        g_f8_pairs[dev].store(n < di->sm_count / 2 ? n : di->sm_count / 2, std::memory_order_relaxed);
-        g_f8_attr_set[dev].store(true, std::memory_order_release);
-    }
+    const Fp8Device* dev = fp8_device(di);
+    if (!dev) return SLIM_ERR_CUDA;
     Fp8Params p = {};
     p.Y = Y; p.Xs = Xs; p.Ws = Ws; p.status = status_dev; p.b = b; p.d_out = d_out; p.groups = ceil_div(d_in, kF8Group);
-    if (b > 128) {
-        const int pairs = g_f8_pairs[dev].load(std::memory_order_relaxed);
-        const long long t256 = (long long)ceil_div(b, 256) * ceil_div(d_out, 256), t128 = (long long)ceil_div(b, 256) * ceil_div(d_out, 128);
-        return (t256 + pairs - 1) / pairs * 4 <= (t128 + pairs - 1) / pairs * 3 ? launch_pair8<256>(p, Xq, x_format, Wq, w_format, d_in, pairs, st)
-                                                                              : launch_pair8<128>(p, Xq, x_format, Wq, w_format, d_in, pairs, st);
+    const Fp8Plan plan = fp8_plan(b, d_out, p.groups, di->sm_count, dev->pairs, dev->clusters);
+    switch (plan.kernel) {
+    case FP8_CLUSTER_16:  return launch_small8<16>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, st);
+    case FP8_CLUSTER_32:  return launch_small8<32>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, st);
+    case FP8_CLUSTER_64:  return launch_small8<64>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, st);
+    case FP8_CLUSTER_128: return launch_small8<128>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, st);
+    case FP8_ROWS_32:     return launch_tokens8<32, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
+    case FP8_ROWS_64:     return launch_tokens8<64, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
+    case FP8_ROWS_128:    return launch_tokens8<128, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
+    case FP8_PAIR_128:    return launch_tokens8<128, true>(p, Xq, x_format, Wq, w_format, d_in, dev->pairs, st);
+    case FP8_PAIR_256:    return launch_tokens8<256, true>(p, Xq, x_format, Wq, w_format, d_in, dev->pairs, st);
     }
-    return b <= 16   ? launch_small8<16>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st)
-           : b <= 32 ? launch_small8<32>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st)
-           : b <= 64 ? launch_small8<64>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st)
-                     : launch_small8<128>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
+    return SLIM_ERR_UNSUPPORTED_SHAPE;
 }
 
 }  // namespace slim
