@@ -157,47 +157,6 @@ __device__ __forceinline__ void store_frag(__nv_bfloat16* Y, int d_out, int row,
     }
 }
 
-// A warp's walk over `count` groups from `first` on: the scales of a tile's tokens (32 a lane and step, EACH steps at most) times the
-// block's, into the slots of a ring, of which `before` uses came before.  AHEAD groups' loads are under way while the ones before are handed over.
-template <int EACH, int AHEAD, int SLOTS>
-__device__ __forceinline__ void bring_scales(const float* Xs, const float* ws, int groups, int first, int count, int n0, int b, int each, uint32_t ring, uint32_t slot_bytes,
-                                             uint64_t* full, uint64_t* empty, int before, int lane, volatile uint32_t* abort_flag)
-{
-    float v[AHEAD][EACH], w[AHEAD];
-    auto load = [&](int i0) {
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const bool in = i0 + j < count;
-            w[j] = in ? ws[first + i0 + j] : 0.f;
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                const int n = n0 + lane + 32 * e;
-                v[j][e] = in && e < each && n < b ? Xs[(size_t)n * groups + first + i0 + j] : 0.f;
-            }
-        }
-    };
-    load(0);
-    for (int i0 = 0; i0 < count; i0 += AHEAD) {
-        float s[AHEAD][EACH];
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) s[j][e] = v[j][e] * w[j];
-        load(i0 + AHEAD);
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const int g = before + i0 + j, slot = g % SLOTS;
-            if (i0 + j >= count) break;
-            if (g >= SLOTS) warp_wait(&empty[slot], ((g / SLOTS) & 1) ^ 1, abort_flag);
-#pragma unroll
-            for (int e = 0; e < EACH; ++e)
-                if (e < each && (uint32_t)(lane + 32 * e) * 4 < slot_bytes) sts32(ring + slot * slot_bytes + (lane + 32 * e) * 4, s[j][e]);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&full[slot]);
-        }
-    }
-}
-
 }  // namespace f8
 
 struct alignas(128) Fp8Params {
@@ -206,23 +165,28 @@ struct alignas(128) Fp8Params {
     uint32_t* status;
     int b, d_out, groups;
     uint32_t idesc;
+    int ahead;
 };
 
 // ---------------------------------------------------------------- a cluster for 128 rows: few tokens
 // The C CTAs of a cluster cut the groups of columns into C ranges; each makes the partial tile of 128 rows x N tokens of its range, and
 // they exchange them once at the end: 128 / C rows to each, added up in the CTAs' order.
+// A wait, a load and an arrival take longer than a group's few tokens: kBatch groups are handed over at a time, side by side in tensor memory
+// (one token, 4096 -> 4096 in one CTA a tile, a group at a time: 0.24 us a group).
 // Warps: 0-3 accumulate (32 rows each), 4 requests tiles by TMA, 5 issues MMAs, 6 brings the scales.
+// Up to 32 tokens a CTA takes less than half of an SM's shared memory, and two are there at once: while one exchanges, the other streams.
 template <int N> struct SmallCfg8 {
     static constexpr int kThreads = 7 * 32;
     static constexpr int kCtasPerSm = N <= 32 ? 2 : 1;
-    static constexpr int kStages = N <= 16 ? 5 : N == 32 ? 4 : N == 64 ? 6 : 4;
+    static constexpr int kStages = N <= 16 ? 5 : N == 32 ? 4 : N == 64 ? 7 : 4;
     static constexpr int kStage = kF8Group * (kF8Group + N);             // the weight's tile, then the tokens'
-    static constexpr int kBuffers = N <= 64 ? 4 : 2, kTmemCols = kBuffers * N;
-    static constexpr int kSlots = N <= 64 ? 8 : 4;                       // groups whose scales are there
-    static constexpr int kChunk = N < 32 ? N : 32;                       // tokens read from tensor memory at once
-    static constexpr int kOffRecv = kStages * kStage, kOffScales = kOffRecv + N * 512, kOffBars = kOffScales + kSlots * N * 4;
+    static constexpr int kBatch = N <= 16 ? 4 : N <= 64 ? 2 : 1, kCols = kBatch * N;      // groups of a batch; its columns of tensor memory
+    static constexpr int kSets = 2, kTmemCols = kSets * kCols;           // batches in tensor memory
+    static constexpr int kSlots = 4;                                     // batches whose scales are there
+    static constexpr int kChunk = 32;                                    // columns read from tensor memory at once
+    static constexpr int kOffRecv = kStages * kStage, kOffScales = kOffRecv + N * 512, kOffBars = kOffScales + kSlots * kCols * 4;
     static constexpr size_t kSmem = 1024 + kOffBars + 256;
-    static_assert(kSmem <= (kCtasPerSm == 2 ? 113 : 227) * 1024, "shared memory");
+    static_assert(kSmem <= (kCtasPerSm == 2 ? 113 : 227) * 1024 && (2 * kStages + 2 * kSets + 2 * kSlots + 1) * 8 + 8 <= 256, "shared memory");
 };
 
 template <int N>
@@ -231,15 +195,15 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
 {
     using namespace f8;
     using Cfg = SmallCfg8<N>;
-    constexpr int kStages = Cfg::kStages, kBuffers = Cfg::kBuffers, kSlots = Cfg::kSlots, kAtoms = N / 8;
+    constexpr int kStages = Cfg::kStages, kBatch = Cfg::kBatch, kCols = Cfg::kCols, kSets = Cfg::kSets, kSlots = Cfg::kSlots, kAtoms = N / 8;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + Cfg::kOffBars);      // [kStages] tiles landed
     uint64_t* empty = full + kStages;                // [kStages] the MMAs that read the stage are complete
-    uint64_t* acc_full = empty + kStages;            // [kBuffers] a group's MMAs are complete
-    uint64_t* acc_empty = acc_full + kBuffers;       // [kBuffers] four warps have read the buffer
-    uint64_t* sc_full = acc_empty + kBuffers;        // [kSlots]
-    uint64_t* sc_empty = sc_full + kSlots;           // [kSlots]
+    uint64_t* acc_full = empty + kStages;            // [kSets] a batch's MMAs are complete
+    uint64_t* acc_empty = acc_full + kSets;          // [kSets] four warps have read the batch
+    uint64_t* sc_full = acc_empty + kSets;           // [kSlots] a batch's scales are there
+    uint64_t* sc_empty = sc_full + kSlots;           // [kSlots] four warps have read them
     uint64_t* recv_full = sc_empty + kSlots;         // the cluster's partial tiles have come
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(recv_full + 1);
     volatile uint32_t* abort_flag = tmem_slot + 1;
@@ -255,7 +219,7 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
-        for (int i = 0; i < kBuffers; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
+        for (int i = 0; i < kSets; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
         for (int i = 0; i < kSlots; ++i) { mbar_init(&sc_full[i], 1); mbar_init(&sc_empty[i], 4); }
         mbar_init(recv_full, 1);
         *abort_flag = 0u;
@@ -271,6 +235,10 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
     __syncthreads();
     fence_after_sync();
     if (ctas > 1) cluster_arrive();                  // this CTA's barriers are there; waited for before the first remote store
+    // The weight's first tiles are asked into the L2 while the grid before still runs (which reads nothing: what that grid may write to them is
+    // seen), where all CTAs have an SM of their own: one token, 4096 -> 4096 6.15 us -> 5.6, but 13824 -> 5120, 160 CTAs, 14.6 -> 16.1.
+    if (p.ahead && warp == 4 && elect_one())
+        for (int i = 0; i < min(n_groups, kStages); ++i) prefetch_tile(&tmW, (g0 + i) * kF8Group, m0);
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(tmem_slot), 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -278,45 +246,106 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
 
     if (warp == 4) {
         // ============================ tiles ============================
-        for (int i = 0; i < n_groups; ++i) {
+        auto request = [&](int i) {
             const int st = i % kStages;
-            if (i >= kStages) warp_wait(&empty[st], ((i / kStages) & 1) ^ 1, abort_flag);
             unsigned char* at = smem + st * Cfg::kStage;
-            if (elect_one()) {
-                mbar_expect_tx(&full[st], Cfg::kStage);
-                tma_tile(at, &tmW, (g0 + i) * kF8Group, m0, &full[st]);
-                tma_tile(at + kF8Group * kF8Group, &tmX, (g0 + i) * kF8Group, n0, &full[st]);
-            }
+            mbar_expect_tx(&full[st], Cfg::kStage);
+            tma_tile(at, &tmW, (g0 + i) * kF8Group, m0, &full[st]);
+            tma_tile(at + kF8Group * kF8Group, &tmX, (g0 + i) * kF8Group, n0, &full[st]);
+        };
+        if (elect_one())
+            for (int i = 0; i < min(n_groups, kStages); ++i) request(i);
+        __syncwarp();
+        for (int i = kStages; i < n_groups; ++i) {
+            warp_wait(&empty[i % kStages], ((i / kStages) & 1) ^ 1, abort_flag);
+            if (elect_one()) request(i);
+            __syncwarp();
         }
     } else if (warp == 5) {
         // ============================ MMA issue ============================
-        for (int i = 0; i < n_groups; ++i) {
-            const int st = i % kStages, buf = i % kBuffers;
-            warp_wait(&full[st], (i / kStages) & 1, abort_flag);
-            if (i >= kBuffers) warp_wait(&acc_empty[buf], ((i / kBuffers) & 1) ^ 1, abort_flag);
-            fence_after_sync();
-            const uint32_t a = desc_lo(s32(smem + st * Cfg::kStage)), x = a + (kF8Group * kF8Group >> 4), d = tmem_base + buf * N;
-            if (elect_one()) {
+        // Two groups at a time: what the warp spends on a group is barriers' answers and the way in and out of its elected lane (16 tokens,
+        // 8192 -> 28672 41.7 us -> 39.4; the requests stay apart: a stage is asked for as soon as it is free).
+        for (int i = 0; i < n_groups; i += 2) {
+            const bool two = i + 1 < n_groups;
+            const int st0 = i % kStages, st1 = (i + 1) % kStages;
+            // (batches of one group: the second one's buffer is asked for behind the first one's MMAs)
+            auto buffer = [&](int k) {
+                const int batch = k / kBatch, set = batch % kSets;
+                if (k % kBatch == 0 && batch >= kSets) warp_wait(&acc_empty[set], ((batch / kSets) & 1) ^ 1, abort_flag);
+            };
+            auto issue = [&](int k, int st) {
+                const int set = (k / kBatch) % kSets, u = k % kBatch;
+                const uint32_t a = desc_lo(s32(smem + st * Cfg::kStage)), x = a + (kF8Group * kF8Group >> 4), d = tmem_base + set * kCols + u * N;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) mma_f8(d, a + 2 * j, x + 2 * j, p.idesc, j > 0 ? 1u : 0u);       // 32 columns each
+                if (u + 1 == kBatch || k + 1 == n_groups) mma_commit(&acc_full[set]);
                 mma_commit(&empty[st]);
-                mma_commit(&acc_full[buf]);
+            };
+            buffer(i);
+            if (two) warp_wait2(&full[st0], (i / kStages) & 1, &full[st1], ((i + 1) / kStages) & 1, abort_flag);
+            else     warp_wait(&full[st0], (i / kStages) & 1, abort_flag);
+            fence_after_sync();
+            if (kBatch > 1) {
+                if (elect_one()) {
+                    issue(i, st0);
+                    if (two) issue(i + 1, st1);
+                }
+            } else {
+                if (elect_one()) issue(i, st0);
+                if (two) {
+                    buffer(i + 1);
+                    fence_after_sync();
+                    if (elect_one()) issue(i + 1, st1);
+                }
             }
+            __syncwarp();
         }
     } else if (warp == 6) {
-        // ============================ scales: of the tokens times the block's ============================
-        bring_scales<(N + 31) / 32, 4, kSlots>(p.Xs, p.Ws + (size_t)tile * p.groups, p.groups, g0, n_groups, n0, p.b, (N + 31) / 32, s32(smem + Cfg::kOffScales), N * 4,
-                                               sc_full, sc_empty, 0, lane, abort_flag);
+        // ============================ scales: of the tokens times the block's, [group of a batch][token] ============================
+        constexpr int kEach = kCols / 32, kAhead = 2;
+        const float* ws = p.Ws + (size_t)tile * p.groups + g0;
+        const int batches = ceil_div(n_groups, kBatch);
+        float v[kAhead][kEach], w[kAhead][kEach];
+        auto load = [&](int k0) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    const int at = lane + 32 * e, i = (k0 + k) * kBatch + at / N, n = n0 + at % N;
+                    const bool in = i < n_groups && n < p.b;
+                    v[k][e] = in ? p.Xs[(size_t)n * p.groups + g0 + i] : 0.f;
+                    w[k][e] = in ? ws[i] : 0.f;
+                }
+        };
+        load(0);
+        for (int k0 = 0; k0 < batches; k0 += kAhead) {
+            float s[kAhead][kEach];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) s[k][e] = v[k][e] * w[k][e];
+            load(k0 + kAhead);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int batch = k0 + k, slot = batch % kSlots;
+                if (batch >= batches) break;
+                if (batch >= kSlots) warp_wait(&sc_empty[slot], ((batch / kSlots) & 1) ^ 1, abort_flag);
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) sts32(s32(smem + Cfg::kOffScales) + (slot * kCols + lane + 32 * e) * 4, s[k][e]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sc_full[slot]);
+            }
+        }
     } else {
         // ============================ accumulation ============================
-        constexpr int kA = Cfg::kChunk / 8, kChunks = N / Cfg::kChunk;
+        constexpr int kA = Cfg::kChunk / 8, kChunks = kCols / Cfg::kChunk;
         unsigned long long acc[2][kAtoms][2] = {};               // 16 rows each: pairs of tokens of rows r and r + 8
-        for (int i = 0; i < n_groups; ++i) {
-            const int buf = i % kBuffers, slot = i % kSlots;
-            warp_wait2(&acc_full[buf], (i / kBuffers) & 1, &sc_full[slot], (i / kSlots) & 1, abort_flag);
+        for (int i = 0, batch = 0; i < n_groups; i += kBatch, ++batch) {
+            const int set = batch % kSets, slot = batch % kSlots;
+            warp_wait2(&acc_full[set], (batch / kSets) & 1, &sc_full[slot], (batch / kSlots) & 1, abort_flag);
             fence_after_sync();
-            const uint32_t t = tmem_base + ((uint32_t)(warp * 32) << 16) + buf * N;
-            const uint32_t sc = s32(smem + Cfg::kOffScales) + slot * N * 4 + (lane & 3) * 8;
+            const uint32_t t = tmem_base + ((uint32_t)(warp * 32) << 16) + set * kCols;
+            const uint32_t sc = s32(smem + Cfg::kOffScales) + slot * kCols * 4 + (lane & 3) * 8;
             Frag<kA> f[2][2];
             tmem_ld(t, f[0][0]);
             tmem_ld(t + (16u << 16), f[0][1]);
@@ -329,21 +358,23 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
                 } else {
                     fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&acc_empty[buf]);
+                    if (elect_one()) mbar_arrive(&acc_empty[set]);
                 }
 #pragma unroll
                 for (int a = 0; a < kA; ++a) {
-                    const unsigned long long s = lds64(sc + (c * kA + a) * 32);
+                    const int col = c * Cfg::kChunk + a * 8, at = (col % N) / 8;
+                    if (kBatch > 1 && i + col / N >= n_groups) continue;             // no such group: what the columns hold is none of this call's
+                    const unsigned long long s = lds64(sc + col * 4);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const float* v = f[c & 1][h].v[a];
-                        fma2(acc[h][c * kA + a][0], v[0], v[1], s);
-                        fma2(acc[h][c * kA + a][1], v[2], v[3], s);
+                        fma2(acc[h][at][0], v[0], v[1], s);
+                        fma2(acc[h][at][1], v[2], v[3], s);
                     }
                 }
             }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sc_empty[slot]);
+            if (elect_one()) mbar_arrive(&sc_empty[slot]);
         }
         const int row = m0 + (lane >> 2), token = n0 + (lane & 3) * 2;
         if (ctas == 1) {
@@ -693,14 +724,17 @@ static int resident_clusters(K kernel, int ctas, int threads, size_t smem) {
     return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess ? n : 0;
 }
 template <typename K>
-static bool large_smem(K kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess; }
+static bool large_smem(K kernel, size_t bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+}
 
 template <int N>
 static bool prepare_small8(int (&clusters)[4]) {
     using Cfg = SmallCfg8<N>;
     if (!large_smem(fp8_small_kernel<N>, Cfg::kSmem)) return false;
+    // (the occupancy query says one CTA an SM for every kernel with tensor memory, however little shared memory it has)
     for (int i = 0; i < 4; ++i)
-        if ((clusters[i] = resident_clusters(fp8_small_kernel<N>, 1 << i, Cfg::kThreads, Cfg::kSmem)) < 1) return false;
+        if ((clusters[i] = Cfg::kCtasPerSm * resident_clusters(fp8_small_kernel<N>, 1 << i, Cfg::kThreads, Cfg::kSmem)) < 1) return false;
     return true;
 }
 template <int N, bool PAIR>
@@ -728,12 +762,13 @@ static const Fp8Device* fp8_device(const DeviceInfo* di) {
 }
 
 template <int N>
-static slim_status_t launch_small8(Fp8Params p, const void* Xq, int x_format, const void* Wq, int w_format, int d_in, int ctas, cudaStream_t st) {
+static slim_status_t launch_small8(Fp8Params p, const void* Xq, int x_format, const void* Wq, int w_format, int d_in, int ctas, int sm_count, cudaStream_t st) {
     using Cfg = SmallCfg8<N>;
     p.idesc = f8::idesc_f8(kF8Group, N, w_format, x_format);
     CUtensorMap tmW, tmX;
     if (!f8_map(&tmW, Wq, d_in, p.d_out, kF8Group) || !f8_map(&tmX, Xq, d_in, p.b, N)) return SLIM_ERR_CUDA;
     const int tiles = ceil_div(p.d_out, kF8Group), token_tiles = ceil_div(p.b, N);
+    p.ahead = (long long)tiles * token_tiles * ctas <= sm_count;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * ctas), (unsigned)token_tiles); cfg.blockDim = dim3(Cfg::kThreads); cfg.dynamicSmemBytes = Cfg::kSmem; cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -791,10 +826,10 @@ slim_status_t launch_fp8(const uint8_t* Xq, const float* Xs, int x_format, int b
     p.Y = Y; p.Xs = Xs; p.Ws = Ws; p.status = status_dev; p.b = b; p.d_out = d_out; p.groups = ceil_div(d_in, kF8Group);
     const Fp8Plan plan = fp8_plan(b, d_out, p.groups, di->sm_count, dev->pairs, dev->clusters);
     switch (plan.kernel) {
-    case FP8_CLUSTER_16:  return launch_small8<16>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, st);
-    case FP8_CLUSTER_32:  return launch_small8<32>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, st);
-    case FP8_CLUSTER_64:  return launch_small8<64>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, st);
-    case FP8_CLUSTER_128: return launch_small8<128>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, st);
+    case FP8_CLUSTER_16:  return launch_small8<16>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
+    case FP8_CLUSTER_32:  return launch_small8<32>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
+    case FP8_CLUSTER_64:  return launch_small8<64>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
+    case FP8_CLUSTER_128: return launch_small8<128>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
     case FP8_ROWS_32:     return launch_tokens8<32, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
     case FP8_ROWS_64:     return launch_tokens8<64, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
     case FP8_ROWS_128:    return launch_tokens8<128, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
