@@ -85,16 +85,21 @@ __device__ __forceinline__ void tmem_wait(Frag<A>& f, Frag<A>& g) {
     }
 }
 
-// 16 columns of this thread's row of a buffer; the wait as above.
-__device__ __forceinline__ void tmem_ld_row(uint32_t taddr, float (&r)[16]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+// 32 columns of this thread's row of a buffer; the wait as above.
+__device__ __forceinline__ void tmem_ld_row(uint32_t taddr, float (&r)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
-                   "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]) : "r"(taddr) : "memory");
+                   "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]),
+                   "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]),
+                   "=f"(r[24]), "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31]) : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void tmem_wait_row(float (&r)[16]) {
+__device__ __forceinline__ void tmem_wait_row(float (&r)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
                    "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]) :: "memory");
+    asm volatile("" : "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]),
+                      "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31]));
 }
 
 // acc += v * s, for two neighbouring columns.
@@ -513,7 +518,7 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
     if (warp < kWarps) {
         if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(Cfg::kRegs));
         // ============================ accumulation, then a tile's end ============================
-        constexpr int kChunks = kCols / 16;
+        constexpr int kChunks = kCols / 32;
         const int side = warp >> 2, quarter = warp & 3;
         const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + side * kCols;
         const uint32_t out = s32(smem + Cfg::kOffOut) + warp * Cfg::kOutSlot, give = PAIR ? peer_addr(acc_empty, 0) : 0u;
@@ -540,21 +545,21 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
                 const uint32_t ta = t0 + buf * kBufferCols;
                 warp_wait(&acc_full[buf], (g / kBuffers) & 1, abort_flag);
                 fence_after_sync();
-                float f[2][16];
+                float f[2][32];
                 tmem_ld_row(ta, f[0]);
                 const unsigned long long s = pair_of(s4.x, s4.x);
                 s4.x = s4.y; s4.y = s4.z; s4.z = s4.w;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
                     tmem_wait_row(f[c & 1]);
-                    if (c + 1 < kChunks) tmem_ld_row(ta + (c + 1) * 16, f[(c + 1) & 1]);
+                    if (c + 1 < kChunks) tmem_ld_row(ta + (c + 1) * 32, f[(c + 1) & 1]);
                     else {
                         fence_before_sync();
                         __syncwarp();
                         if (elect_one()) { if (PAIR) mbar_arrive_remote(give + buf * 8); else mbar_arrive(&acc_empty[buf]); }
                     }
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) fma2(acc[c * 8 + k], f[c & 1][2 * k], f[c & 1][2 * k + 1], s);
+                    for (int k = 0; k < 16; ++k) fma2(acc[c * 16 + k], f[c & 1][2 * k], f[c & 1][2 * k + 1], s);
                 }
             }
             // 64 rows of the weight (32) at a time into the warp's place in shared memory, [token][64 rows] bf16, 128-byte (64-byte) swizzle,
