@@ -202,6 +202,26 @@ def test_linear_against_64_bits(b, d_in, d_out):
     assert torch.equal(Y, K.slim_linear_fwd_fp8(*o, status=status)) and int(status) == 0
 
 
+# Each kernel with several tiles a CTA or pair, columns that end inside a block, four or eight groups, and rows of Y that are and are not a
+# multiple of 16 bytes; the tokens that its tile has.
+KERNELS = [(16, 1040, 1030, 16), (16, 8192, 300, 16), (9, 2064, 9000, 16), (30, 656, 260, 32), (30, 8192, 300, 32), (25, 2064, 9001, 32), (64, 6000, 9000, 64),
+           (50, 400, 100, 64), (128, 8192, 16, 128), (200, 8192, 1030, 128), (100, 14208, 4480, 128), (2100, 5120, 100, 128), (70, 144, 16, 128),
+           (520, 144, 100, 128), (3000, 400, 1001, 128), (200, 2064, 5120, 256), (3000, 2064, 513, 256), (520, 1728, 8200, 256), (200, 1040, 9999, 256),
+           (1500, 1040, 2050, 256), (520, 1728, 4100, 256), (2100, 3600, 1030, 256), (1100, 512, 20000, 256)]
+
+
+@pytest.mark.parametrize("b, d_in, d_out, tokens", KERNELS)
+def test_every_kernel_of_the_linear_layer(b, d_in, d_out, tokens):
+    o = operands(b, d_in, d_out, 3 * b + d_in)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    Y = K.slim_linear_fwd_fp8(*o, status=status)
+    assert K.slim_last_token_tile() == tokens and K.slim_last_launch_count() == 1
+    check_linear(*o, Y)
+    for _ in range(5):
+        assert torch.equal(Y, K.slim_linear_fwd_fp8(*o, status=status))
+    assert int(status) == 0
+
+
 @pytest.mark.parametrize("x, w", [(E4, E5), (E5, E4), (E5, E5)])
 @pytest.mark.parametrize("b, d_in, d_out", [(1, 1024, 400), (16, 656, 512), (64, 2048, 320), (130, 1040, 640), (700, 1728, 1100)])
 def test_linear_formats(b, d_in, d_out, x, w):
@@ -398,3 +418,45 @@ def test_bad_tensors_leave_the_device_usable():
         K.slim_linear_fwd_fp8(None, None, None, None)
     o = operands(4, 256, 128, 0)
     check_linear(*o, K.slim_linear_fwd_fp8(*o))
+
+
+def test_first_call_of_a_process_in_a_capture():
+    """What a call sets up once per device does not disturb a capture."""
+    import os
+    import subprocess
+    import sys
+    code = (
+        "import torch\n"
+        "from paper_2410_09615_b200 import binding as K\n"
+        "X = torch.randn(200, 512, device='cuda').bfloat16(); W = torch.randn(300, 512, device='cuda')\n"
+        "gamma = torch.ones(512, device='cuda').bfloat16()\n"
+        "K.native(); torch.cuda.synchronize()\n"
+        "def f():\n"
+        "    Wp = K.slim_pack_fp8(W)\n"
+        "    return [K.slim_linear_fwd_fp8(*K.slim_rmsnorm_fp8(X[:b], gamma, 1e-5, X[:b])[:2], *Wp) for b in (1, 20, 50, 200)]\n"
+        "g = torch.cuda.CUDAGraph()\n"
+        "with torch.cuda.graph(g):\n"
+        "    got = f()\n"
+        "g.replay(); torch.cuda.synchronize()\n"
+        "assert all(torch.equal(a, b) for a, b in zip(got, f())); print('ok')\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and out.stdout.strip() == "ok", out.stderr[-2000:]
+
+
+def test_calls_on_two_threads():
+    import threading
+    o = [operands(b, 1040, 700, b) for b in (8, 300)]
+    refs = [K.slim_linear_fwd_fp8(*x) for x in o]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(100):
+                if not torch.equal(K.slim_linear_fwd_fp8(*o[i]), refs[i]):
+                    bad.append(i)
+
+    threads = [threading.Thread(target=work, args=(i % 2,)) for i in range(4)]
+    [t.start() for t in threads], [t.join() for t in threads]
+    assert not bad
