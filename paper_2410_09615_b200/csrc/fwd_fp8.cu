@@ -85,7 +85,7 @@ __device__ __forceinline__ void tmem_wait(Frag<A>& f, Frag<A>& g) {
     }
 }
 
-// 32 columns of this thread's row of a buffer; the wait as above.
+// 32 or 16 columns of this thread's row of a buffer; the wait as above.
 __device__ __forceinline__ void tmem_ld_row(uint32_t taddr, float (&r)[32]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
                  "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
@@ -100,6 +100,17 @@ __device__ __forceinline__ void tmem_wait_row(float (&r)[32]) {
                    "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]) :: "memory");
     asm volatile("" : "+f"(r[16]), "+f"(r[17]), "+f"(r[18]), "+f"(r[19]), "+f"(r[20]), "+f"(r[21]), "+f"(r[22]), "+f"(r[23]),
                       "+f"(r[24]), "+f"(r[25]), "+f"(r[26]), "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31]));
+}
+
+__device__ __forceinline__ void tmem_ld_row(uint32_t taddr, float (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]),
+                   "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_row(float (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(r[0]), "+f"(r[1]), "+f"(r[2]), "+f"(r[3]), "+f"(r[4]), "+f"(r[5]), "+f"(r[6]), "+f"(r[7]),
+                   "+f"(r[8]), "+f"(r[9]), "+f"(r[10]), "+f"(r[11]), "+f"(r[12]), "+f"(r[13]), "+f"(r[14]), "+f"(r[15]) :: "memory");
 }
 
 // acc += v * s, for two neighbouring columns.
@@ -438,6 +449,9 @@ template <int N, bool PAIR> struct TokCfg8 {
     static constexpr int kWarps = PAIR ? 8 : 4, kThreads = (kWarps + 4) * 32;            // .. kWarps tiles, + 1 MMAs, + 2 scales
     static constexpr int kRegs = 216, kOtherRegs = 72;                                  // pairs: 2 x 216 + 72 = 3 x 168, what the three warpgroups are launched with
     static constexpr int kSides = PAIR ? 2 : 1, kCols = N / kSides;                     // columns of a warp
+    // Columns read at once: more give a buffer back earlier (pairs, 256 rows: 660 cycles a group, 680 with 16), where the registers hold them
+    // (128 rows a warp and no share of the other warps' registers: 100 tokens, 8192 -> 8192 22.3 us with 16, 27.7 with 32).
+    static constexpr int kChunk = !PAIR && N == 128 ? 16 : 32;
     static constexpr int kRowsW = PAIR ? N / 2 : N;                                     // of the weight that a CTA loads
     static constexpr int kOffW = kF8Group * kF8Group, kStage = kOffW + kRowsW * kF8Group, kStages = 163840 / kStage;
     static constexpr int kBufferCols = N <= 128 ? 128 : 256, kBuffers = 512 / kBufferCols;
@@ -518,7 +532,7 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
     if (warp < kWarps) {
         if (PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(Cfg::kRegs));
         // ============================ accumulation, then a tile's end ============================
-        constexpr int kChunks = kCols / 32;
+        constexpr int kChunk = Cfg::kChunk, kChunks = kCols / kChunk;
         const int side = warp >> 2, quarter = warp & 3;
         const uint32_t t0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + side * kCols;
         const uint32_t out = s32(smem + Cfg::kOffOut) + warp * Cfg::kOutSlot, give = PAIR ? peer_addr(acc_empty, 0) : 0u;
@@ -545,21 +559,21 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
                 const uint32_t ta = t0 + buf * kBufferCols;
                 warp_wait(&acc_full[buf], (g / kBuffers) & 1, abort_flag);
                 fence_after_sync();
-                float f[2][32];
+                float f[2][kChunk];
                 tmem_ld_row(ta, f[0]);
                 const unsigned long long s = pair_of(s4.x, s4.x);
                 s4.x = s4.y; s4.y = s4.z; s4.z = s4.w;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
                     tmem_wait_row(f[c & 1]);
-                    if (c + 1 < kChunks) tmem_ld_row(ta + (c + 1) * 32, f[(c + 1) & 1]);
+                    if (c + 1 < kChunks) tmem_ld_row(ta + (c + 1) * kChunk, f[(c + 1) & 1]);
                     else {
                         fence_before_sync();
                         __syncwarp();
                         if (elect_one()) { if (PAIR) mbar_arrive_remote(give + buf * 8); else mbar_arrive(&acc_empty[buf]); }
                     }
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) fma2(acc[c * 16 + k], f[c & 1][2 * k], f[c & 1][2 * k + 1], s);
+                    for (int k = 0; k < kChunk / 2; ++k) fma2(acc[c * (kChunk / 2) + k], f[c & 1][2 * k], f[c & 1][2 * k + 1], s);
                 }
             }
             // 64 rows of the weight (32) at a time into the warp's place in shared memory, [token][64 rows] bf16, 128-byte (64-byte) swizzle,
