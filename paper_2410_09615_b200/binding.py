@@ -103,8 +103,9 @@ def native():
         spec.loader.exec_module(m)
         m.bind(SlimError, *[ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value for name in
                             ("slim_linear_fwd_ex", "slim_linear_fwd_tiled", "slim_linear_fwd_q", "slim_tiled_bytes", "slim_strerror",
-                             "slim_pack", "slim_quant", "slim_quant_workspace_bytes", "slim_mask_top2", "slim_pack_adapter", "slim_rmsnorm", "slim_rmsnorm_fp8", "slim_quant_fp8",
-                             "slim_pack_fp8", "slim_linear_fwd_fp8")])
+                             "slim_pack", "slim_quant", "slim_quant_workspace_bytes", "slim_mask_top2", "slim_pack_adapter")])
+        m.bind_fp8(*[ctypes.cast(getattr(lib(), name), ctypes.c_void_p).value for name in
+                     ("slim_rmsnorm", "slim_rmsnorm_fp8", "slim_quant_fp8", "slim_pack_fp8", "slim_linear_fwd_fp8")])
         _native = m
     return _native
 

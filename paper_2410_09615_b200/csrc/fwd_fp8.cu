@@ -189,10 +189,10 @@ struct alignas(128) Fp8Params {
 // they exchange them once at the end: 128 / C rows to each, added up in the CTAs' order.
 // A wait, a load and an arrival take longer than a group's few tokens: kBatch groups are handed over at a time, side by side in tensor memory
 // (one token, 4096 -> 4096 in one CTA a tile, a group at a time: 0.24 us a group).
-// Warps: 0-3 accumulate (32 rows each), 4 requests tiles by TMA, 5 issues MMAs, 6 brings the scales.
+// Warps: 0-3 accumulate (32 rows each), 4 and 7 request tiles by TMA, 5 issues MMAs, 6 brings the scales.
 // Up to 32 tokens a CTA takes less than half of an SM's shared memory, and two are there at once: while one exchanges, the other streams.
 template <int N> struct SmallCfg8 {
-    static constexpr int kThreads = 7 * 32;
+    static constexpr int kThreads = 8 * 32;
     static constexpr int kCtasPerSm = N <= 32 ? 2 : 1;
     static constexpr int kStages = N <= 16 ? 5 : N == 32 ? 4 : N == 64 ? 7 : 4;
     static constexpr int kStage = kF8Group * (kF8Group + N);             // the weight's tile, then the tokens'
@@ -260,14 +260,17 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("fence.proxy.async;" ::: "memory");            // what the grid before wrote is read through TMA
 
-    if (warp == 4) {
+    if (warp == 4 || warp == 7) {
         // ============================ tiles ============================
+        // The weight's by one warp, the tokens' by another: a request takes its warp about 100 ns.
+        const bool weight = warp == 4;
         auto request = [&](int i) {
             const int st = i % kStages;
             unsigned char* at = smem + st * Cfg::kStage;
-            mbar_expect_tx(&full[st], Cfg::kStage);
-            tma_tile(at, &tmW, (g0 + i) * kF8Group, m0, &full[st]);
-            tma_tile(at + kF8Group * kF8Group, &tmX, (g0 + i) * kF8Group, n0, &full[st]);
+            if (weight) {
+                mbar_expect_tx(&full[st], Cfg::kStage);          // (bytes that land before are counted below zero)
+                tma_tile(at, &tmW, (g0 + i) * kF8Group, m0, &full[st]);
+            } else tma_tile(at + kF8Group * kF8Group, &tmX, (g0 + i) * kF8Group, n0, &full[st]);
         };
         if (elect_one())
             for (int i = 0; i < min(n_groups, kStages); ++i) request(i);
@@ -442,11 +445,11 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
 // Tokens are the MMA's rows here: a thread has one token, so the product of a group's scales is one number for each 128 rows of the
 // weight, and the buffer is read with tcgen05.ld 32x32b, 64 words a cycle and quarter of the SM (16x256b: 16, so that a buffer of
 // 128 x 256 took as long to read as to multiply).
-// Warps: 0-7 accumulate (32 tokens x half of the rows each), 8 requests tiles by TMA, 9 issues MMAs, 10 brings the scales.
+// Warps: 0-7 accumulate (32 tokens x half of the rows each), 8 and 11 request tiles by TMA, 9 issues MMAs, 10 brings the scales.
 // PAIR false: single CTAs on tiles of 128 tokens x N rows (32, 64 or 128), for layers whose pair tiles would leave most SMs without one; a warp
 // then accumulates all rows of its 32 tokens.
 template <int N, bool PAIR> struct TokCfg8 {
-    static constexpr int kWarps = PAIR ? 8 : 4, kThreads = (kWarps + 4) * 32;            // .. kWarps tiles, + 1 MMAs, + 2 scales
+    static constexpr int kWarps = PAIR ? 8 : 4, kThreads = (kWarps + 4) * 32;            // .. kWarps and + 3 tiles, + 1 MMAs, + 2 scales
     static constexpr int kRegs = 216, kOtherRegs = 72;                                  // pairs: 2 x 216 + 72 = 3 x 168, what the three warpgroups are launched with
     static constexpr int kSides = PAIR ? 2 : 1, kCols = N / kSides;                     // columns of a warp
     // Columns read at once: more give a buffer back earlier (pairs, 256 rows: 660 cycles a group, 680 with 16), where the registers hold them
@@ -625,8 +628,10 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     } else {
         if (PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(Cfg::kOtherRegs));
-        if (warp == kWarps) {
-            // ============================ tiles ============================
+        if (warp == kWarps || warp == kWarps + 3) {
+            // ============================ tiles: the tokens', the weight's ============================
+            // A warp each: a request takes its warp about 100 ns, as long as a narrow tile's MMAs.
+            const bool tokens = warp == kWarps;
             int g = 0;
             for (int t = first_tile; t < tiles; t += units) {
                 const Tile ti = tile_of(t);
@@ -635,15 +640,16 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
                     if (g >= kStages) warp_wait(&empty[st], ((g / kStages) & 1) ^ 1, abort_flag);
                     unsigned char* at = smem + st * Cfg::kStage;
                     if (elect_one()) {
-                        // (the odd CTA's bytes are counted on the even one's barrier too, which cannot end the phase before it has announced all)
-                        if (rank == 0) mbar_expect_tx(&full[st], (uint32_t)(kCtas * Cfg::kStage));
-                        if (PAIR) {
-                            const uint32_t bar = peer_addr(&full[st], 0);
-                            tma_tile_pair(at, &tmX, i * kF8Group, ti.m0, bar);
-                            tma_tile_pair(at + Cfg::kOffW, &tmW, i * kF8Group, ti.n0 + (int)rank * Cfg::kRowsW, bar);
+                        // (bytes that land before they are announced, the odd CTA's among them, are counted below zero: the phase cannot end
+                        // without the announcement)
+                        const uint32_t bar = PAIR ? peer_addr(&full[st], 0) : 0u;
+                        if (tokens) {
+                            if (rank == 0) mbar_expect_tx(&full[st], (uint32_t)(kCtas * Cfg::kStage));
+                            if (PAIR) tma_tile_pair(at, &tmX, i * kF8Group, ti.m0, bar);
+                            else      tma_tile(at, &tmX, i * kF8Group, ti.m0, &full[st]);
                         } else {
-                            tma_tile(at, &tmX, i * kF8Group, ti.m0, &full[st]);
-                            tma_tile(at + Cfg::kOffW, &tmW, i * kF8Group, ti.n0, &full[st]);
+                            if (PAIR) tma_tile_pair(at + Cfg::kOffW, &tmW, i * kF8Group, ti.n0 + (int)rank * Cfg::kRowsW, bar);
+                            else      tma_tile(at + Cfg::kOffW, &tmW, i * kF8Group, ti.n0, &full[st]);
                         }
                     }
                 }

@@ -101,7 +101,7 @@ PyObject* finish(int code, PyObject* y, const char* where) {
 }
 
 bool bound(Py_ssize_t given, Py_ssize_t wanted) {
-    if (!g_fwd) { PyErr_SetString(PyExc_RuntimeError, "bind() has not been called"); return false; }
+    if (!g_fwd || !g_fwd8) { PyErr_SetString(PyExc_RuntimeError, "bind() and bind_fp8() have not been called"); return false; }
     if (given == wanted) return true;
     PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
     return false;
@@ -531,8 +531,8 @@ PyObject* linear_fwd_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // bind(SlimError, addresses of the functions in the loaded libslim)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject* err;
-    unsigned long long f, t, q, by, tx, pk, qu, qb, mk, pa, rn, r8, q8, p8, f8;
-    if (!PyArg_ParseTuple(args, "OKKKKKKKKKKKKKKK", &err, &f, &t, &q, &by, &tx, &pk, &qu, &qb, &mk, &pa, &rn, &r8, &q8, &p8, &f8)) return nullptr;
+    unsigned long long f, t, q, by, tx, pk, qu, qb, mk, pa;
+    if (!PyArg_ParseTuple(args, "OKKKKKKKKKK", &err, &f, &t, &q, &by, &tx, &pk, &qu, &qb, &mk, &pa)) return nullptr;
     Py_INCREF(err);
     Py_XDECREF(g_error);
     g_error = err;
@@ -540,13 +540,21 @@ PyObject* bind(PyObject*, PyObject* args) {
     g_tiled_bytes = reinterpret_cast<BytesFn>(by); g_text = reinterpret_cast<TextFn>(tx);
     g_pack = reinterpret_cast<PackFn>(pk); g_quant = reinterpret_cast<QuantFn>(qu); g_quant_bytes = reinterpret_cast<QuantBytesFn>(qb);
     g_mask = reinterpret_cast<MaskFn>(mk); g_pack_adapter = reinterpret_cast<AdapterFn>(pa);
-    g_norm = reinterpret_cast<NormFn>(rn); g_norm8 = reinterpret_cast<Norm8Fn>(r8); g_quant8 = reinterpret_cast<Quant8Fn>(q8);
+    Py_RETURN_NONE;
+}
+
+// bind_fp8(addresses of the norms, the 8-bit quantisers and the 8-bit layer in the loaded libslim), behind bind()
+PyObject* bind_fp8(PyObject*, PyObject* args) {
+    unsigned long long n, n8, q8, p8, f8;
+    if (!PyArg_ParseTuple(args, "KKKKK", &n, &n8, &q8, &p8, &f8)) return nullptr;
+    g_norm = reinterpret_cast<NormFn>(n); g_norm8 = reinterpret_cast<Norm8Fn>(n8); g_quant8 = reinterpret_cast<Quant8Fn>(q8);
     g_pack8 = reinterpret_cast<Pack8Fn>(p8); g_fwd8 = reinterpret_cast<Fwd8Fn>(f8);
     Py_RETURN_NONE;
 }
 
 PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, nullptr},
+    {"bind_fp8", bind_fp8, METH_VARARGS, nullptr},
     {"linear_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(linear_fwd)), METH_FASTCALL, nullptr},
     {"linear_fwd_tiled", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(linear_fwd_tiled)), METH_FASTCALL, nullptr},
     {"linear_fwd_q", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(linear_fwd_q)), METH_FASTCALL, nullptr},

@@ -460,3 +460,36 @@ def test_calls_on_two_threads():
     threads = [threading.Thread(target=work, args=(i % 2,)) for i in range(4)]
     [t.start() for t in threads], [t.join() for t in threads]
     assert not bad
+
+
+def test_other_threads_run_during_a_call(tmp_path):
+    """The calls give the interpreter to other threads: a stand-in for the library's function returns only when another thread has run
+    (or, with an error, after a second)."""
+    import ctypes
+    import subprocess
+    import threading
+    import time
+    src, so = tmp_path / "stall.c", tmp_path / "stall.so"
+    src.write_text("#include <time.h>\nvolatile int go = 0;\nint stall(void) {\n    struct timespec nap = {0, 1000000};\n"
+                   "    for (int i = 0; i < 1000; ++i) { if (go) return 0; nanosleep(&nap, 0); }\n    return 6;\n}\n")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", str(src), "-o", str(so)], check=True)
+    stand_in = ctypes.CDLL(str(so))
+    go = ctypes.c_int.in_dll(stand_in, "go")
+    addr = lambda f: ctypes.cast(f, ctypes.c_void_p).value       # noqa: E731
+    own = [addr(getattr(K.lib(), n)) for n in ("slim_rmsnorm", "slim_rmsnorm_fp8", "slim_quant_fp8", "slim_pack_fp8", "slim_linear_fwd_fp8")]
+    o, X, gamma = operands(2, 128, 128, 0), rows(2, 128), torch.ones(128, device="cuda").bfloat16()
+    native = K.native()
+    try:
+        native.bind_fp8(*[addr(stand_in.stall)] * 5)
+        for call in (lambda: K.slim_rmsnorm(X, gamma, 1e-5), lambda: K.slim_rmsnorm_fp8(X, gamma, 1e-5), lambda: K.slim_quant_fp8(X),
+                     lambda: K.slim_pack_fp8(X), lambda: K.slim_linear_fwd_fp8(*o)):
+            go.value = 0
+            other = threading.Thread(target=lambda: (time.sleep(0.02), setattr(go, "value", 1)))
+            other.start()
+            try:
+                call()                                           # raises where the other thread could not run
+            finally:
+                other.join()
+    finally:
+        native.bind_fp8(*own)
+    check_linear(*o, K.slim_linear_fwd_fp8(*o))
