@@ -54,7 +54,7 @@ extern "C" {
 typedef enum {
     SLIM_OK = 0,
     SLIM_ERR_INVALID_ARG = 1,        /* null / misaligned pointer, b < 1, negative size, scale not finite */
-    SLIM_ERR_UNSUPPORTED_SHAPE = 2,  /* d_in % 64, d_out % 16 or r % 16 not zero */
+    SLIM_ERR_UNSUPPORTED_SHAPE = 2,  /* a size that the call does not take: d_in % 64, d_out % 16 or r % 16 not zero (8-bit operands: columns % 16) */
     SLIM_ERR_BAD_MASK = 3,           /* device: more than two kept values in a group */
     SLIM_ERR_CODE_RANGE = 4,         /* device: kept code outside [-8, 7] */
     SLIM_ERR_WORKSPACE = 5,          /* workspace NULL or smaller than slim_workspace_bytes */

@@ -457,7 +457,7 @@ const char* slim_strerror(slim_status_t status)
     switch (status) {
     case SLIM_OK: return "ok";
     case SLIM_ERR_INVALID_ARG: return "invalid argument (null or misaligned pointer, bad size)";
-    case SLIM_ERR_UNSUPPORTED_SHAPE: return "unsupported shape (d_in % 64, d_out % 16, r % 16 must be 0)";
+    case SLIM_ERR_UNSUPPORTED_SHAPE: return "unsupported shape (d_in % 64, d_out % 16, r % 16 must be 0; 8-bit operands: columns % 16, a norm up to 32768 of them)";
     case SLIM_ERR_BAD_MASK: return "a 2:4 group keeps more than two values";
     case SLIM_ERR_CODE_RANGE: return "a kept code lies outside [-8, 7]";
     case SLIM_ERR_WORKSPACE: return "workspace missing or too small";

@@ -3,12 +3,19 @@
 //
 // The inner sums are tcgen05.mma (kind::f8f6f4, fp32 accumulate) of one group of 128 columns each, into a tensor-memory buffer of its
 // own; the outer sum is made in registers: warps read a group's buffer, multiply it with the group's two scales and add it to their
-// fp32 accumulators, while the next groups' MMAs run.  The weight's 128 rows of a block are the MMA's rows (M), so the block's scale is one
-// number for a whole CTA; tokens are its columns (N).
+// fp32 accumulators, while the next groups' MMAs run.  (A scale is any binary32 number, so it cannot ride in the MMA, whose block scales are
+// powers of two.)
 //
-// Registers of a group's tile: tcgen05.ld 16x256b gives a lane, of every 16 rows x 8 tokens, rows r = lane / 4 and r + 8 and tokens
-// c = 2 (lane % 4) and c + 1: four values, two pairs of tokens, so that a lane needs the scales of a quarter of the tokens (as pairs, the
-// operand of fma.f32x2) instead of all of them.
+// Two kernels, which differ in what the MMA's rows (M) are; fp8_plan.h picks one and its tile:
+//   fp8_small_kernel   few tokens.  The weight's 128 rows of a block are the MMA's rows, so that none is empty; the tokens are its columns.
+//                      Clusters cut the columns of the layer among their CTAs.  Bound by the weight's stream from the HBM, or by one
+//                      launch's chain: first bytes, MMAs, exchange.
+//   fp8_tokens_kernel  more tokens, as the MMA's rows: a thread has one token, and a group's scales are one number for it.  Persistent CTA
+//                      pairs on tiles of 256 tokens, or single CTAs on 128.  Bound by the hand-over of the two buffers of 256 columns
+//                      that tensor memory holds (MMAs 513 cycles, reading 350, and the way between the two), and by the power limit.
+//
+// What the loops' waits cost decides both, so they are written for it: a warp's lanes stay together (warp_wait), nothing behind a barrier's
+// answer is spilled, remote arrivals have no cluster scope (1100 cycles where they had).
 #include <atomic>
 #include <mutex>
 #include "fp8.cuh"
@@ -185,10 +192,13 @@ struct alignas(128) Fp8Params {
 };
 
 // ---------------------------------------------------------------- a cluster for 128 rows: few tokens
+// Registers of a batch's tile: tcgen05.ld 16x256b gives a lane, of every 16 rows x 8 tokens, rows r = lane / 4 and r + 8 and tokens
+// c = 2 (lane % 4) and c + 1: four values, two pairs of tokens, so that a lane needs the scales of a quarter of the tokens (as pairs, the
+// operand of fma.f32x2) instead of all of them.  The block's scale is one number for the whole CTA.
 // The C CTAs of a cluster cut the groups of columns into C ranges; each makes the partial tile of 128 rows x N tokens of its range, and
 // they exchange them once at the end: 128 / C rows to each, added up in the CTAs' order.
 // A wait, a load and an arrival take longer than a group's few tokens: kBatch groups are handed over at a time, side by side in tensor memory
-// (one token, 4096 -> 4096 in one CTA a tile, a group at a time: 0.24 us a group).
+// (one token, 4096 -> 4096, a CTA a tile: 10.1 us a group at a time, 9.6 so).
 // Warps: 0-3 accumulate (32 rows each), 4 and 7 request tiles by TMA, 5 issues MMAs, 6 brings the scales.
 // Up to 32 tokens a CTA takes less than half of an SM's shared memory, and two are there at once: while one exchanges, the other streams.
 template <int N> struct SmallCfg8 {
@@ -439,7 +449,7 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
 }
 
 // ---------------------------------------------------------------- pairs of CTAs: many tokens
-// Persistent clusters of two CTAs walk tiles of 256 tokens x up to 256 rows (n, a multiple of 64) with cta_group::2 MMAs that the even CTA
+// Persistent clusters of two CTAs walk tiles of 256 tokens x N rows (128 or 256) with cta_group::2 MMAs that the even CTA
 // issues: each CTA loads its own 128 tokens and half of the tile's rows, and accumulates its 128 tokens.  All rings run on across
 // tiles, so the next tile's groups are multiplied while this tile is stored.
 // Tokens are the MMA's rows here: a thread has one token, so the product of a group's scales is one number for each 128 rows of the
