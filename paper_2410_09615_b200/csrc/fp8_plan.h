@@ -3,12 +3,14 @@
 // Up to 64 tokens a cluster has 128 rows and cuts the columns: the weight's stream has to be spread over the SMs, and the tokens are the
 // MMA's columns, so that no row of it is empty.  Above, the kernels differ in the tile that a CTA or a pair has, and the call takes the one
 // with the shortest time by
-//     fixed + rounds of tiles * groups of 128 columns in a tile's walk * time of a group,
+//     fixed + the longer of  rounds of tiles * groups of 128 columns in a tile's walk * time of a group
+//                       and  the tiles' bytes at the 11.7 TB/s that the SMs together got from the L2,
 // with the measured fixed times and times of a group below (ns, weights in rotation).  Measured against it, us (tokens, columns -> rows):
 //     100, 8192 -> 8192   tiles of 64 rows 20.1, cluster 20.2, pairs of 128 rows 20.7, 128 rows 22.3, pairs of 256 28.4, 32 rows 33.7
 //     100, 5120 -> 13824  128 rows 17.1, cluster 20.3, pairs of 256 20.8, 64 rows 24.4, pairs of 128 24.4, 32 rows 31.7
 //     333, 8192 -> 1024   cluster 12.9, 32 rows 18.8, pairs of 128 19.1, 64 rows 19.6, 128 rows 21.1, pairs of 256 27.6
 //     333, 8192 -> 8192   pairs of 256 31.4, pairs of 128 37.5, 128 rows 41.3, 64 rows 52.4, cluster 64.2, 32 rows 94.1
+//     600, 8192 -> 8192   pairs of 128 rows 53.8, pairs of 256 59.9, 128 rows 60.7, 64 rows 84.7, 32 rows 140
 //     4000, 512 -> 512    128 rows 4.2, 64 rows 5.0, pairs of 128 5.3, pairs of 256 5.9, 32 rows 6.6
 #pragma once
 
@@ -46,7 +48,9 @@ inline Fp8Plan fp8_plan(int b, int d_out, int groups, int sms, int pairs, const 
     const Tile kinds[] = {{FP8_ROWS_32, 128, 32, 3200, 230}, {FP8_ROWS_64, 128, 64, 3200, 250}, {FP8_ROWS_128, 128, 128, 3000, 300},
                           {FP8_PAIR_128, 256, 128, 3500, 270}, {FP8_PAIR_256, 256, 256, 4300, 420}};
     for (const Tile& k : kinds) {
-        const long long cost = k.fixed + up(up(b, k.tokens) * up(d_out, k.rows), k.tokens == 256 ? pairs : sms) * groups * k.group;
+        const long long n = up(b, k.tokens) * up(d_out, k.rows);
+        const long long walk = up(n, k.tokens == 256 ? pairs : sms) * groups * k.group, feed = (long long)((double)n * groups * (k.tokens + k.rows) * 128 / 11700);
+        const long long cost = k.fixed + (walk > feed ? walk : feed);
         if (cost < least) { least = cost; best = {k.kernel, 1}; }
     }
     return best;
