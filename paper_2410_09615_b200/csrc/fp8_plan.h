@@ -1,17 +1,22 @@
 // Which kernel serves a call of the 8-bit layer (fwd_fp8.cu), as plain C++: the host's side of it, and what the tests go over.
 //
 // Up to 64 tokens a cluster has 128 rows and cuts the columns: the weight's stream has to be spread over the SMs, and the tokens are the
-// MMA's columns, so that no row of it is empty.  Above, the kernels differ in the tile that a CTA or a pair has, and the call takes the one
-// with the shortest time by
-//     fixed + the longer of  rounds of tiles * groups of 128 columns in a tile's walk * time of a group
-//                       and  the tiles' bytes at the 11.7 TB/s that the SMs together got from the L2,
-// with the measured fixed times and times of a group below (ns, weights in rotation).  Measured against it, us (tokens, columns -> rows):
-//     100, 8192 -> 8192   tiles of 64 rows 20.1, cluster 20.2, pairs of 128 rows 20.7, 128 rows 22.3, pairs of 256 28.4, 32 rows 33.7
-//     100, 5120 -> 13824  128 rows 17.1, cluster 20.3, pairs of 256 20.8, 64 rows 24.4, pairs of 128 24.4, 32 rows 31.7
-//     333, 8192 -> 1024   cluster 12.9, 32 rows 18.8, pairs of 128 19.1, 64 rows 19.6, 128 rows 21.1, pairs of 256 27.6
-//     333, 8192 -> 8192   pairs of 256 31.4, pairs of 128 37.5, 128 rows 41.3, 64 rows 52.4, cluster 64.2, 32 rows 94.1
-//     600, 8192 -> 8192   pairs of 128 rows 53.8, pairs of 256 59.9, 128 rows 60.7, 64 rows 84.7, 32 rows 140
-//     4000, 512 -> 512    128 rows 4.2, 64 rows 5.0, pairs of 128 5.3, pairs of 256 5.9, 32 rows 6.6
+// MMA's columns, so that no row of it is empty.  The kernels differ in the tile that a CTA, a cluster or a pair has, and from 33 tokens on the
+// call takes the one with the shortest time by the longer of
+//     fixed + rounds of tiles * groups of 128 columns in a tile's walk * time of a group
+//         (rounds * all of it where a CTA ends with its tile, in a cluster)
+//     and the tiles' bytes at the 11.7 TB/s that the SMs together got from the L2,
+// with the fixed times and times of a group below (ns), fitted to 57 measured sizes (weights in rotation): its choice was the fastest or within
+// 1 % of it on 50 of them, and at most 9 % slower.  Some measured, us (tokens, columns -> rows; c: a cluster's tokens, r: a CTA's rows, p: a pair's):
+//     40, 8192 -> 1024    c32 6.3, c64 6.9, c128 7.6, r32 17.7
+//     64, 5120 -> 13824   c64 16.5, r128 16.8, c32 19.0, c128 20.6, r64 24.0, r32 31.8
+//     100, 4096 -> 1024   c32 5.6, c64 6.9, c128 8.2, r32 10.1, r64 10.8, p128 10.9, r128 12.0, p256 15.5
+//     100, 8192 -> 8192   r64 20.0, p128 20.5, c128 21.1, c64 21.4, r128 22.3, c32 24.4, p256 27.8, r32 33.6
+//     231, 8192 -> 1024   c32 10.0, c64 10.1, c128 12.7, r32 17.9, p128 18.4, r64 18.9, r128 21.0, p256 27.0
+//     333, 8192 -> 1024   c128 13.1, c32 14.1, c64 14.4, r32 18.2, p128 18.5, r64 19.0, r128 21.1, p256 27.1
+//     4000, 512 -> 512    r128 4.2, r64 4.8, p128 5.2, p256 5.8, r32 6.4, c128 7.5, c32 8.8, c64 9.7
+//     333, 8192 -> 8192   p256 31.4, p128 37.5, r128 41.3, r64 52.4, c128 64.2, r32 94.1
+//     600, 8192 -> 8192   p128 53.8, p256 59.9, r128 60.7, r64 84.7, r32 140
 #pragma once
 
 namespace slim {
@@ -36,21 +41,29 @@ inline int fp8_cluster_ctas(long long tiles, int groups, const int (&clusters)[4
 inline Fp8Plan fp8_plan(int b, int d_out, int groups, int sms, int pairs, const int (&clusters)[4][4]) {
     auto up = [](long long a, long long n) { return (a + n - 1) / n; };
     const long long blocks = up(d_out, 128);
-    if (b <= 64) {
-        const int i = b <= 16 ? 0 : b <= 32 ? 1 : 2;
-        return {(Fp8Kernel)(FP8_CLUSTER_16 + i), fp8_cluster_ctas(blocks, groups, clusters[i])};
+    if (b <= 32) return {b <= 16 ? FP8_CLUSTER_16 : FP8_CLUSTER_32, fp8_cluster_ctas(blocks, groups, clusters[b <= 16 ? 0 : 1])};
+    auto feed = [](long long tiles, int groups, int tokens, int rows) { return (long long)((double)tiles * groups * (tokens + rows) * 128 / 11700); };
+    Fp8Plan best = {FP8_PAIR_256, 1};
+    long long least = 1ll << 62;
+    struct Cluster { Fp8Kernel kernel; int tokens; long long alone, together, group; };      // (fixed times of one CTA and of several)
+    const Cluster cuts[] = {{FP8_CLUSTER_32, 32, 2250, 3750, 360}, {FP8_CLUSTER_64, 64, 3000, 5000, 300}, {FP8_CLUSTER_128, 128, 4500, 6500, 450}};
+    for (const Cluster& k : cuts) {
+        const long long parts = up(b, k.tokens), tiles = blocks * parts;
+        const int (&resident)[4] = clusters[k.kernel - FP8_CLUSTER_16];
+        const int ctas = fp8_cluster_ctas(tiles, groups, resident);
+        const long long rounds = up(tiles, resident[ctas == 1 ? 0 : ctas == 2 ? 1 : ctas == 4 ? 2 : 3]);
+        const long long walk = rounds * ((ctas > 1 ? k.together : k.alone) + up(groups, ctas) * k.group), bytes = feed(tiles, groups, k.tokens, 128);
+        const long long cost = walk > bytes ? walk : bytes;
+        if (cost < least && parts <= 65535) { least = cost; best = {k.kernel, ctas}; }       // (the grid has a row for each part of the tokens)
     }
-    const long long tiles = blocks * up(b, 128);
-    const int ctas = fp8_cluster_ctas(tiles, groups, clusters[3]);
-    Fp8Plan best = {FP8_CLUSTER_128, ctas};          // (its grid has a row for 128 tokens)
-    long long least = up(b, 128) > 65535 ? (1ll << 62) : (ctas > 1 ? 6500 : 3000) + up(tiles, clusters[3][ctas == 1 ? 0 : ctas == 2 ? 1 : ctas == 4 ? 2 : 3]) * up(groups, ctas) * 440;
+    if (b <= 64) return best;
     struct Tile { Fp8Kernel kernel; int tokens, rows; long long fixed, group; };
-    const Tile kinds[] = {{FP8_ROWS_32, 128, 32, 3200, 230}, {FP8_ROWS_64, 128, 64, 3200, 250}, {FP8_ROWS_128, 128, 128, 3000, 300},
+    const Tile kinds[] = {{FP8_ROWS_32, 128, 32, 2400, 240}, {FP8_ROWS_64, 128, 64, 2500, 255}, {FP8_ROWS_128, 128, 128, 3000, 300},
                           {FP8_PAIR_128, 256, 128, 3500, 270}, {FP8_PAIR_256, 256, 256, 4300, 420}};
     for (const Tile& k : kinds) {
         const long long n = up(b, k.tokens) * up(d_out, k.rows);
-        const long long walk = up(n, k.tokens == 256 ? pairs : sms) * groups * k.group, feed = (long long)((double)n * groups * (k.tokens + k.rows) * 128 / 11700);
-        const long long cost = k.fixed + (walk > feed ? walk : feed);
+        const long long walk = k.fixed + up(n, k.tokens == 256 ? pairs : sms) * groups * k.group, bytes = k.fixed + feed(n, groups, k.tokens, k.rows);
+        const long long cost = walk > bytes ? walk : bytes;
         if (cost < least) { least = cost; best = {k.kernel, 1}; }
     }
     return best;

@@ -31,7 +31,7 @@ int main() {
                     if (!cluster && p.ctas != 1) fail("a cluster of a kernel without", b, n, g, p);
                     if (p.ctas > g) fail("a CTA without columns", b, n, g, p);
                     const int most[4] = {16, 32, 64, 128};
-                    if (b <= 64 && (!cluster || b > most[p.kernel])) fail("more tokens than the kernel has", b, n, g, p);
+                    if ((b <= 16) != (p.kernel == FP8_CLUSTER_16) || (b <= 32 && p.kernel > FP8_CLUSTER_32) || (b <= 64 && !cluster)) fail("another kernel than few tokens have", b, n, g, p);
                     if (cluster && p.ctas > 1) {
                         const int i = p.ctas == 2 ? 1 : p.ctas == 4 ? 2 : 3;
                         const long long tiles = (long long)((n + 127ll) / 128) * ((b + most[p.kernel] - 1ll) / most[p.kernel]);

@@ -204,9 +204,10 @@ def test_linear_against_64_bits(b, d_in, d_out):
 
 # Each kernel with several tiles a CTA or pair, columns that end inside a block, four or eight groups, and rows of Y that are and are not a
 # multiple of 16 bytes; the tokens that its tile has.
-KERNELS = [(16, 1040, 1030, 16), (16, 8192, 300, 16), (9, 2064, 9000, 16), (30, 656, 260, 32), (30, 8192, 300, 32), (25, 2064, 9001, 32), (64, 6000, 9000, 64),
-           (50, 400, 100, 64), (128, 8192, 16, 128), (200, 8192, 1030, 128), (100, 14208, 4480, 128), (2100, 5120, 100, 128), (70, 144, 16, 128),
-           (520, 144, 100, 128), (3000, 400, 1001, 128), (200, 2064, 5120, 256), (3000, 2064, 513, 256), (520, 1728, 8200, 256), (200, 1040, 9999, 256),
+KERNELS = [(16, 1040, 1030, 16), (16, 8192, 300, 16), (9, 2064, 9000, 16), (30, 656, 260, 32), (30, 8192, 300, 32), (25, 2064, 9001, 32),
+           (64, 6000, 9000, 64), (50, 400, 100, 32), (128, 8192, 16, 32), (200, 8192, 1030, 32), (100, 14208, 4480, 64), (2100, 5120, 100, 32),
+           (70, 144, 16, 128), (520, 144, 100, 128), (333, 8192, 1030, 128), (130, 8208, 1930, 128), (64, 1728, 5121, 32), (230, 2064, 4100, 128),
+           (3000, 400, 1001, 128), (200, 2064, 5120, 256), (3000, 2064, 513, 256), (520, 1728, 8200, 256), (200, 1040, 9999, 256),
            (1500, 1040, 2050, 256), (520, 1728, 4100, 256), (2100, 3600, 1030, 256), (1100, 512, 20000, 256)]
 
 
