@@ -363,7 +363,8 @@ size_t slim_noalloc_scratch_needed(int b, int d_out, int d_in, int r);
  * the others 0 (so every product with the group is NaN).
  *
  * Shapes: rows >= 1; columns a multiple of 16 (else SLIM_ERR_UNSUPPORTED_SHAPE), at least 16.  All pointers are DEVICE pointers, 16-byte aligned; those
- * of scales may be 4-byte aligned (rows of a larger batch).  Nothing here needs a workspace or keeps state between calls.
+ * of scales may be 4-byte aligned (rows of a larger batch).  An output overlaps no input, but for H below; the quantisers and the layer take up to
+ * 2^31 - 512 of each size (else SLIM_ERR_INVALID_ARG).  Nothing here needs a workspace or keeps state between calls.
  */
 typedef enum { SLIM_FP8_E4M3 = 0, SLIM_FP8_E5M2 = 1 } slim_fp8_t;
 typedef enum { SLIM_TYPE_BF16 = 0, SLIM_TYPE_F32 = 1 } slim_type_t;
@@ -375,7 +376,7 @@ typedef enum { SLIM_TYPE_BF16 = 0, SLIM_TYPE_F32 = 1 } slim_type_t;
  *   H [b, d] bf16 (out, may be NULL): h, the residual of the next step; it may be X or residual itself;
  *   Y [b, d] bf16 (out): y, the input of slim_linear_fwd and its like.
  * Everything is computed in binary32, from the unrounded h; H and Y are rounded once.  (A row whose sum of squares passes 3.4e38 comes out as zeros.)
- * d <= 32768 (else SLIM_ERR_UNSUPPORTED_SHAPE).  Y must not overlap an input.
+ * d <= 32768 (else SLIM_ERR_UNSUPPORTED_SHAPE).
  */
 slim_status_t slim_rmsnorm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, void* H, void* Y, void* cuda_stream);
 
@@ -393,8 +394,8 @@ slim_status_t slim_pack_fp8(const void* W, slim_type_t type, int d_out, int d_in
  * The forward of a layer whose weight is held in 8 bits (Sec. 2 Eq. 1):
  *     Y[m][n] = sum over groups g of  Xs[m][g] * Ws[n / 128][g] * (sum over the columns k of g of Xq[m][k] Wq[n][k])
  * Inner sums are made by the tensor cores, which accumulate in binary32; a group's sum is scaled and added to the others in binary32;
- * Y [b, d_out] bf16 is rounded once (nearest even).  Bit-identical from run to run.  The product of the two scales of a group must be a
- * finite binary32 number.
+ * Y [b, d_out] bf16 is rounded once (nearest even).  Bit-identical from run to run (another b may sum in another order).  The product of the
+ * two scales of a group must be a finite binary32 number.
  *   Xq [b, d_in] codes, Xs [b, ceil(d_in / 128)], Wq [d_out, d_in] codes, Ws [ceil(d_out / 128), ceil(d_in / 128)]; the formats may differ.
  * Shape rules: b >= 1, d_in % 16 == 0, d_out >= 1 (any).
  */

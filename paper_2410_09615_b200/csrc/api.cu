@@ -390,6 +390,7 @@ slim_status_t slim_linear_fwd_host(const void* X_host, int b, const uint8_t* val
 }
 
 static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static bool too_long(int n) { return n > 0x7FFFFE00; }              // what is rounded up to whole tiles stays below 2^31
 static bool is_fp8(int format) { return format == SLIM_FP8_E4M3 || format == SLIM_FP8_E5M2; }
 
 static slim_status_t check_norm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, const void* H) {
@@ -420,7 +421,7 @@ slim_status_t slim_rmsnorm_fp8(const void* X, const void* residual, const void* 
 slim_status_t slim_quant_fp8(const void* X, int b, int d, slim_fp8_t format, void* codes, float* scales, void* cuda_stream)
 {
     reset_launch_count();
-    if (!X || !codes || !scales || b < 1 || d < 1 || !is_fp8(format)) return SLIM_ERR_INVALID_ARG;
+    if (!X || !codes || !scales || b < 1 || d < 1 || too_long(d) || !is_fp8(format)) return SLIM_ERR_INVALID_ARG;
     if (d % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(X) || !aligned16(codes) || !aligned4(scales)) return SLIM_ERR_INVALID_ARG;
     return launch_quant_fp8(X, b, d, format, codes, scales, (cudaStream_t)cuda_stream);
@@ -429,7 +430,7 @@ slim_status_t slim_quant_fp8(const void* X, int b, int d, slim_fp8_t format, voi
 slim_status_t slim_pack_fp8(const void* W, slim_type_t type, int d_out, int d_in, slim_fp8_t format, void* codes, float* scales, void* cuda_stream)
 {
     reset_launch_count();
-    if (!W || !codes || !scales || d_out < 1 || d_in < 1 || !is_fp8(format) || (type != SLIM_TYPE_BF16 && type != SLIM_TYPE_F32)) return SLIM_ERR_INVALID_ARG;
+    if (!W || !codes || !scales || d_out < 1 || d_in < 1 || too_long(d_out) || too_long(d_in) || !is_fp8(format) || (type != SLIM_TYPE_BF16 && type != SLIM_TYPE_F32)) return SLIM_ERR_INVALID_ARG;
     if (d_in % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(W) || !aligned16(codes) || !aligned4(scales)) return SLIM_ERR_INVALID_ARG;
     return launch_pack_fp8(W, type, d_out, d_in, format, codes, scales, (cudaStream_t)cuda_stream);
@@ -440,6 +441,7 @@ slim_status_t slim_linear_fwd_fp8(const void* Xq, const float* Xs, slim_fp8_t x_
 {
     reset_launch_count();
     if (!Xq || !Xs || !Wq || !Ws || !Y || b < 1 || d_out < 1 || d_in < 1 || !is_fp8(x_format) || !is_fp8(w_format)) return SLIM_ERR_INVALID_ARG;
+    if (too_long(b) || too_long(d_out) || too_long(d_in)) return SLIM_ERR_INVALID_ARG;
     if (d_in % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(Xq) || !aligned16(Wq) || !aligned16(Y) || !aligned4(Xs) || !aligned4(Ws) || !aligned4(status_dev)) return SLIM_ERR_INVALID_ARG;
     slim_status_t err;

@@ -73,6 +73,12 @@ def test_more_of_each(lib):
     assert norm(lib, Y=P) == INVALID and norm(lib, Y=Q) == INVALID and norm(lib, Y=256, H=256) == INVALID      # an output in place of an input
 
 
+@pytest.mark.parametrize("call, name", [(quant, "d"), (pack, "d_out"), (pack, "d_in"), (linear, "b"), (linear, "d_out"), (linear, "d_in")])
+def test_sizes_whose_tiles_pass_31_bits(lib, call, name):
+    for n in ((1 << 31) - 496, (1 << 31) - 16):
+        assert call(lib, **{name: n}) == INVALID
+
+
 def test_a_missing_device_is_an_error_not_a_fall_back(lib):
     if torch.cuda.is_available():
         pytest.skip("there is a device")
