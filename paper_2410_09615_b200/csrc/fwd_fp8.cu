@@ -20,6 +20,7 @@
 #include <mutex>
 #include "fp8.cuh"
 #include "fp8_plan.h"
+#include "fp8_ring.h"
 #include "tcgen05.cuh"
 
 namespace slim {
@@ -51,20 +52,37 @@ __device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint32_t a_lo, uint
 
 // A warp's bounded wait (tcgen05.cuh's mbar_wait, for lanes that go on together: the vote tells the compiler so, and spares it bringing them
 // together again before every instruction of a whole warp).  One that expires raises the CTA's flag, which ends all others and is looked
-// at at the end.
-__device__ __forceinline__ void warp_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
+// at at the end.  False: it gave up; a loader then asks for no more.  (The issuing warp does not look: its MMAs go on over what the stages hold, one
+// group in the time that such a wait takes, and a branch on the answer took 100 tokens, 8192 -> 8192 from 20.1 us to 22.5.)
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
     for (uint32_t it = 0; it < kPSpinLimit; ++it) {
-        if (__all_sync(0xffffffffu, mbar_try(bar, parity, false))) return;
-        if ((it & 63u) == 63u && __any_sync(0xffffffffu, *abort_flag)) return;
+        if (__all_sync(0xffffffffu, mbar_try(bar, parity, false))) return true;
+        if ((it & 63u) == 63u && __any_sync(0xffffffffu, *abort_flag)) return false;
     }
     *abort_flag = 1u;
+    return false;
 }
-__device__ __forceinline__ void warp_wait2(uint64_t* b0, uint32_t p0, uint64_t* b1, uint32_t p1, volatile uint32_t* abort_flag) {
+__device__ __forceinline__ bool warp_wait2(uint64_t* b0, uint32_t p0, uint64_t* b1, uint32_t p1, volatile uint32_t* abort_flag) {
     for (uint32_t it = 0; it < kPSpinLimit; ++it) {
-        if (__all_sync(0xffffffffu, mbar_try(b0, p0, false) & mbar_try(b1, p1, false))) return;
-        if ((it & 63u) == 63u && __any_sync(0xffffffffu, *abort_flag)) return;
+        if (__all_sync(0xffffffffu, mbar_try(b0, p0, false) & mbar_try(b1, p1, false))) return true;
+        if ((it & 63u) == 63u && __any_sync(0xffffffffu, *abort_flag)) return false;
     }
     *abort_flag = 1u;
+    return false;
+}
+
+// A loader's end: no MMA's completion may arrive in this CTA's shared memory after it has left (fp8_ring.h).
+__device__ __forceinline__ void drain(uint64_t* empty, int requested, int places, volatile uint32_t* abort_flag) {
+#pragma unroll 1
+    for (int i = ring_tail(requested, places); i < requested; ++i)
+        if (!warp_wait(&empty[i % places], (i / places) & 1, abort_flag)) break;
+}
+// The end of a CTA in which a wait gave up: what was started is given a million cycles, where a copy or an MMA takes a few thousand at most, before
+// its shared and tensor memory are another's.
+__device__ __forceinline__ void settle(volatile uint32_t* abort_flag) {
+    if (*abort_flag == 0u) return;
+    for (const long long t0 = clock64(); clock64() - t0 < 1000000ll;) {}
+    __syncthreads();
 }
 
 // 16 rows x 8 A columns of a buffer: four values an eight columns.  The wait names the registers, so nothing that uses them is moved ahead of it.
@@ -282,14 +300,16 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
                 tma_tile(at, &tmW, (g0 + i) * kF8Group, m0, &full[st]);
             } else tma_tile(at + kF8Group * kF8Group, &tmX, (g0 + i) * kF8Group, n0, &full[st]);
         };
+        int i = min(n_groups, kStages);
         if (elect_one())
-            for (int i = 0; i < min(n_groups, kStages); ++i) request(i);
+            for (int k = 0; k < i; ++k) request(k);
         __syncwarp();
-        for (int i = kStages; i < n_groups; ++i) {
-            warp_wait(&empty[i % kStages], ((i / kStages) & 1) ^ 1, abort_flag);
+        for (; i < n_groups; ++i) {
+            if (!warp_wait(&empty[i % kStages], ((i / kStages) & 1) ^ 1, abort_flag)) break;
             if (elect_one()) request(i);
             __syncwarp();
         }
+        drain(empty, i, kStages, abort_flag);
     } else if (warp == 5) {
         // ============================ MMA issue ============================
         // Two groups at a time: what the warp spends on a group is barriers' answers and the way in and out of its elected lane (16 tokens,
@@ -424,7 +444,10 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
                 for (int a = 0; a < kAtoms; ++a)
                     if (a < atoms) st_peer4(dst + a * 512, halves(acc[h][a][0]), halves(acc[h][a][1]), bar);
             }
-            mbar_wait_all(recv_full, 0, true, nullptr, 0, false, nullptr, 0, false, abort_flag);
+            // (a CTA that gave up sends what it has and stays for what the others send)
+            if (!mbar_wait_all(recv_full, 0, true, nullptr, 0, false, nullptr, 0, false, abort_flag))
+                for (uint32_t it = 0; it < kPSpinLimit && !mbar_try(recv_full, 0, true); ++it) {}
+            __syncwarp();
             for (int i = warp; i < shares * atoms; i += 4) {
                 const int piece = i / atoms, a = i - piece * atoms;
                 const uint32_t from = recv + (uint32_t)((piece * kAtoms + a) * 512 + lane * 16);
@@ -442,6 +465,7 @@ fp8_small_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap tmW, con
     fence_before_sync();
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) flag_error(p.status, SLIM_ERR_TIMEOUT);
+    settle(abort_flag);
     if (warp == 5) {
         fence_after_sync();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem_base), "r"(Cfg::kTmemCols) : "memory");
@@ -643,11 +667,12 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
             // A warp each: a request takes its warp about 100 ns, as long as a narrow tile's MMAs.
             const bool tokens = warp == kWarps;
             int g = 0;
-            for (int t = first_tile; t < tiles; t += units) {
+            bool ok = true;
+            for (int t = first_tile; ok && t < tiles; t += units) {
                 const Tile ti = tile_of(t);
                 for (int i = 0; i < p.groups; ++i, ++g) {
                     const int st = g % kStages;
-                    if (g >= kStages) warp_wait(&empty[st], ((g / kStages) & 1) ^ 1, abort_flag);
+                    if (g >= kStages && !(ok = warp_wait(&empty[st], ((g / kStages) & 1) ^ 1, abort_flag))) break;
                     unsigned char* at = smem + st * Cfg::kStage;
                     if (elect_one()) {
                         // (bytes that land before they are announced, the odd CTA's among them, are counted below zero: the phase cannot end
@@ -664,6 +689,8 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
                     }
                 }
             }
+            __syncwarp();
+            drain(empty, g, kStages, abort_flag);
         } else if (warp == kWarps + 1) {
             // ============================ MMA issue: a warp of the even CTA ============================
             if (rank == 0) {
@@ -727,6 +754,7 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
     fence_before_sync();
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) flag_error(p.status, SLIM_ERR_TIMEOUT);
+    settle(abort_flag);
     if (PAIR) cluster_sync_all();                    // neither CTA leaves while the other may still use its shared memory
     if (warp == kWarps + 1) {
         fence_after_sync();
