@@ -393,9 +393,9 @@ slim_status_t slim_pack_fp8(const void* W, slim_type_t type, int d_out, int d_in
 /*
  * The forward of a layer whose weight is held in 8 bits (Sec. 2 Eq. 1):
  *     Y[m][n] = sum over groups g of  Xs[m][g] * Ws[n / 128][g] * (sum over the columns k of g of Xq[m][k] Wq[n][k])
- * Inner sums are made by the tensor cores, which accumulate in binary32; a group's sum is scaled and added to the others in binary32;
- * Y [b, d_out] bf16 is rounded once (nearest even).  Bit-identical from run to run (another b may sum in another order).  The product of the
- * two scales of a group must be a finite binary32 number.
+ * Inner sums are made by the tensor cores, which accumulate in binary32.  The product of the two scales of a group is rounded to binary32 (it must be
+ * finite; below 2^-126 it is a subnormal number, which is kept, so its step is 2^-149); a group's sum is multiplied with it and added to the others in
+ * binary32; Y [b, d_out] bf16 is rounded once (nearest even).  Bit-identical from run to run (another b may sum in another order).
  *   Xq [b, d_in] codes, Xs [b, ceil(d_in / 128)], Wq [d_out, d_in] codes, Ws [ceil(d_out / 128), ceil(d_in / 128)]; the formats may differ.
  * Shape rules: b >= 1, d_in % 16 == 0, d_out >= 1 (any).
  */

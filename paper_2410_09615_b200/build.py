@@ -12,7 +12,9 @@ NATIVE = os.path.join(HERE, "_slim_native.so")
 SOURCES = ["api.cu", "pack.cu", "repack.cu", "fwd_simple.cu", "fwd_small.cu", "fwd_prefill.cu",
            "fwd_noalloc.cu", "adapter_q.cu", "quant_search.cu", "mask.cu", "quant_fp8.cu", "fwd_fp8.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-              "-Xcompiler", "-fPIC", "--use_fast_math"]
+              "-Xcompiler", "-fPIC"]
+# Under --use_fast_math subnormal numbers become zeros.  The 8-bit layer's products of scales and its sums keep them (include/slim.h).
+KEEP_SUBNORMAL = {"fwd_fp8.cu"}
 
 
 def _older(target: str, deps) -> bool:
@@ -20,7 +22,8 @@ def _older(target: str, deps) -> bool:
 
 
 def _stale() -> bool:
-    return _older(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")] + [os.path.join(INCLUDE, "slim.h")])
+    return _older(LIB, [os.path.join(CSRC, f) for f in os.listdir(CSRC) if not f.endswith(".cpp")] +
+                  [os.path.join(INCLUDE, "slim.h"), os.path.abspath(__file__)])
 
 
 def _cudart(torch_root: str):
@@ -68,7 +71,7 @@ def build(force: bool = False, verbose: bool = False, defines=(), out: str | Non
     procs = []
     for src in SOURCES:
         obj = os.path.join(bdir, src.replace(".cu", ".o"))
-        cmd = [nvcc, *NVCC_FLAGS, *[f"-D{d}" for d in defines], "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, src),
+        cmd = [nvcc, *NVCC_FLAGS, *([] if src in KEEP_SUBNORMAL else ["--use_fast_math"]), *[f"-D{d}" for d in defines], "-I", INCLUDE, "-I", CSRC, "-c", os.path.join(CSRC, src),
                "-o", obj]
         if verbose:
             cmd.insert(1, "-Xptxas")

@@ -14,6 +14,8 @@
 //                      pairs on tiles of 256 tokens, or single CTAs on 128.  Bound by the hand-over of the two buffers of 256 columns
 //                      that tensor memory holds (MMAs 513 cycles, reading 350, and the way between the two), and by the power limit.
 //
+// A product of scales below 2^-126 is a subnormal number and counts: this file is compiled without flush-to-zero.
+//
 // What the loops' waits cost decides both, so they are written for it: a warp's lanes stay together (warp_wait), nothing behind a barrier's
 // answer is spilled, remote arrivals have no cluster scope (1100 cycles where they had).
 #include <atomic>
