@@ -375,7 +375,8 @@ typedef enum { SLIM_TYPE_BF16 = 0, SLIM_TYPE_F32 = 1 } slim_type_t;
  *   X [b, d] bf16; residual [b, d] bf16 or NULL (h = x); gamma [d] bf16; eps > 0, finite;
  *   H [b, d] bf16 (out, may be NULL): h, the residual of the next step; it may be X or residual itself;
  *   Y [b, d] bf16 (out): y, the input of slim_linear_fwd and its like.
- * Everything is computed in binary32, from the unrounded h; H and Y are rounded once.  (A row whose sum of squares passes 3.4e38 comes out as zeros.)
+ * Everything is computed in binary32, from the unrounded h; H and Y are rounded once.  (A row whose sum of squares passes 3.4e38 comes out as zeros.
+ * Subnormal numbers are kept, those of eps too; squares and their sums below 2^-126 have a step of 2^-149.)
  * d <= 32768 (else SLIM_ERR_UNSUPPORTED_SHAPE).
  */
 slim_status_t slim_rmsnorm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, void* H, void* Y, void* cuda_stream);

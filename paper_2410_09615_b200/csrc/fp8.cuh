@@ -24,12 +24,15 @@ struct Scale {
     }
 };
 
+// Sums and products that keep subnormal numbers (the library is compiled with flush-to-zero).
+__device__ __forceinline__ float add_rn(float a, float b) { float v; asm("add.rn.f32 %0, %1, %2;" : "=f"(v) : "f"(a), "f"(b)); return v; }
+__device__ __forceinline__ float mul_rn(float a, float b) { float v; asm("mul.rn.f32 %0, %1, %2;" : "=f"(v) : "f"(a), "f"(b)); return v; }
+__device__ __forceinline__ float fma_rn(float a, float b, float c) { float v; asm("fma.rn.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(a), "f"(b), "f"(c)); return v; }
+
 // Two codes, v's in the low byte; rounding to nearest even, magnitudes above the largest number become that.
 template <int FMT>
 __device__ __forceinline__ uint32_t codes2(float v, float w, float inv) {
-    float a, b;
-    asm("mul.rn.f32 %0, %1, %2;" : "=f"(a) : "f"(v), "f"(inv));          // subnormal values are not flushed
-    asm("mul.rn.f32 %0, %1, %2;" : "=f"(b) : "f"(w), "f"(inv));
+    const float a = mul_rn(v, inv), b = mul_rn(w, inv);
     uint16_t c;
     if (FMT == SLIM_FP8_E4M3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(b), "f"(a));
     else                      asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(c) : "f"(b), "f"(a));

@@ -24,8 +24,10 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
 
 // A CTA has a row, a thread V vectors of eight columns of it, in registers from the first load to the last store: h = x + residual is
 // added in binary32 and normalised as it is; only the copy that goes back to the residual stream is rounded.  Sixteen neighbouring
-// threads hold a group of 128 columns.  FMT: the 8-bit format, or -1 for a bf16 output.
-template <int V, int FMT>
+// threads hold a group of 128 columns.  FMT: the 8-bit format, or -1 for a bf16 output.  TINY_EPS: eps is below 2^-64; a sum below 2^-64 and eps
+// are then taken 2^64-fold, which is exact, so that division, sum and root see no subnormal number.  (A larger eps makes the mean square of such a sum
+// what it is; as a question that every call asks, 16 x 8192 into bf16 took 1.96 us instead of 1.91.)
+template <int V, int FMT, bool TINY_EPS>
 __global__ void __launch_bounds__(1024)
 rmsnorm_kernel(const NormParams p)
 {
@@ -52,14 +54,14 @@ rmsnorm_kernel(const NormParams p)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 h[i][2 * k] = bf16_lo(xw[k]); h[i][2 * k + 1] = bf16_hi(xw[k]);
-                if (p.residual) { h[i][2 * k] += bf16_lo(rw[k]); h[i][2 * k + 1] += bf16_hi(rw[k]); }
+                if (p.residual) { h[i][2 * k] = add_rn(h[i][2 * k], bf16_lo(rw[k])); h[i][2 * k + 1] = add_rn(h[i][2 * k + 1], bf16_hi(rw[k])); }
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum = fmaf(h[i][k], h[i][k], sum);
+            for (int k = 0; k < 8; ++k) sum = fma_rn(h[i][k], h[i][k], sum);
         }
     }
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    for (int o = 16; o; o >>= 1) sum = add_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
     if (lane == 0) parts[tid >> 5] = sum;
     if (p.H) {
 #pragma unroll
@@ -72,8 +74,10 @@ rmsnorm_kernel(const NormParams p)
     // every warp adds the parts up itself, in the same order
     sum = lane < ((int)blockDim.x >> 5) ? parts[lane] : 0.f;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const float inv_rms = __frsqrt_rn(__fdiv_rn(sum, (float)p.d) + p.eps);
+    for (int o = 16; o; o >>= 1) sum = add_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
+    float inv_rms;
+    if (TINY_EPS && sum < 0x1p-64f) inv_rms = __frsqrt_rn(__fdiv_rn(mul_rn(sum, 0x1p64f), (float)p.d) + mul_rn(p.eps, 0x1p64f)) * 0x1p32f;
+    else inv_rms = __frsqrt_rn(__fdiv_rn(sum, (float)p.d) + p.eps);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int at = i * blockDim.x + tid;
@@ -84,8 +88,8 @@ rmsnorm_kernel(const NormParams p)
         uint32_t largest = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            y[2 * k] = h[i][2 * k] * inv_rms * bf16_lo(gw[k]);
-            y[2 * k + 1] = h[i][2 * k + 1] * inv_rms * bf16_hi(gw[k]);
+            y[2 * k] = mul_rn(mul_rn(h[i][2 * k], inv_rms), bf16_lo(gw[k]));
+            y[2 * k + 1] = mul_rn(mul_rn(h[i][2 * k + 1], inv_rms), bf16_hi(gw[k]));
             largest = max(largest, max(magnitude(y[2 * k]), magnitude(y[2 * k + 1])));
         }
         if (FMT < 0) {
@@ -111,7 +115,8 @@ static void run_norm(const NormParams& p, int b, int sms, cudaStream_t st)
     // (one row of 4096 1.8 us, with two 2.15; 4096 rows of 8192 37.4 us, with one 47).
     const int v = p.vecs <= 256 || (p.vecs <= 1024 && b <= sms) ? 1 : p.vecs <= 2048 ? 2 : 4;
     const int threads = ceil_div(ceil_div(p.vecs, v), 32) * 32;
-    auto* kernel = v == 1 ? rmsnorm_kernel<1, FMT> : v == 2 ? rmsnorm_kernel<2, FMT> : rmsnorm_kernel<4, FMT>;
+    auto* kernel = p.eps < 0x1p-64f ? (v == 1 ? rmsnorm_kernel<1, FMT, true> : v == 2 ? rmsnorm_kernel<2, FMT, true> : rmsnorm_kernel<4, FMT, true>)
+                                    : (v == 1 ? rmsnorm_kernel<1, FMT, false> : v == 2 ? rmsnorm_kernel<2, FMT, false> : rmsnorm_kernel<4, FMT, false>);
     launch_dependent(kernel, dim3((unsigned)b), dim3((unsigned)threads), 0, st, p);
 }
 

@@ -50,9 +50,9 @@ def test_linear_keeps_subnormal_products_of_scales(b, d_in, d_out, low):
     Xq = torch.randint(-2, 3, (b, d_in), generator=g, device="cuda").float().to(E4)
     Wq = torch.randint(-2, 3, (d_out, d_in), generator=g, device="cuda").float().to(E4)
     G, N = -(-d_in // 128), -(-d_out // 128)
-    one = torch.ones((), dtype=torch.float64, device="cuda")
-    Xs = torch.ldexp(one, -60 - torch.randint(0, 4, (b, G), generator=g, device="cuda")).float()
-    Ws = torch.ldexp(one, low + 60 - torch.randint(0, 4, (N, G), generator=g, device="cuda")).float()
+    ones = lambda r: torch.ones((r, G), dtype=torch.float64, device="cuda")       # noqa: E731
+    Xs = torch.ldexp(ones(b), -60 - torch.randint(0, 4, (b, G), generator=g, device="cuda")).float()
+    Ws = torch.ldexp(ones(N), low + 60 - torch.randint(0, 4, (N, G), generator=g, device="cuda")).float()
     s = product(Xs, Ws, d_out)
     Y = K.slim_linear_fwd_fp8(Xq, Xs, Wq, Ws)
     ref = sums(Xq, Wq, s)
