@@ -363,8 +363,9 @@ size_t slim_noalloc_scratch_needed(int b, int d_out, int d_in, int r);
  * the others 0 (so every product with the group is NaN).
  *
  * Shapes: rows >= 1; columns a multiple of 16 (else SLIM_ERR_UNSUPPORTED_SHAPE), at least 16.  All pointers are DEVICE pointers, 16-byte aligned; those
- * of scales may be 4-byte aligned (rows of a larger batch).  An output overlaps no input, but for H below; the quantisers and the layer take up to
- * 2^31 - 512 of each size (else SLIM_ERR_INVALID_ARG).  Nothing here needs a workspace or keeps state between calls.
+ * of scales may be 4-byte aligned (rows of a larger batch).  An output overlaps no input and no other output, but for H below (norms and quantisers return
+ * SLIM_ERR_INVALID_ARG, the layer where Y begins where an operand does); the quantisers and the layer take up to 2^31 - 512 of each size (else
+ * SLIM_ERR_INVALID_ARG).  Nothing here needs a workspace or keeps state between calls.
  */
 typedef enum { SLIM_FP8_E4M3 = 0, SLIM_FP8_E5M2 = 1 } slim_fp8_t;
 typedef enum { SLIM_TYPE_BF16 = 0, SLIM_TYPE_F32 = 1 } slim_type_t;

@@ -2,6 +2,7 @@
 // per-device attribute cache.  All arithmetic lives in the kernel files.
 #include <atomic>
 #include <cmath>
+#include <initializer_list>
 #include <mutex>
 #include "common.cuh"
 
@@ -393,10 +394,31 @@ static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3
 static bool too_long(int n) { return n > 0x7FFFFE00; }              // what is rounded up to whole tiles stays below 2^31
 static bool is_fp8(int format) { return format == SLIM_FP8_E4M3 || format == SLIM_FP8_E5M2; }
 
+// A tensor's place in memory, and whether two have bytes in common (no place: none).
+struct Place {
+    const void* at;
+    size_t bytes;
+};
+static bool overlap(const Place& a, const Place& b) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a.at), q = reinterpret_cast<uintptr_t>(b.at);
+    return p && q && (p < q ? q - p < a.bytes : p - q < b.bytes);
+}
+static bool overlaps_any(const Place& out, std::initializer_list<Place> others) {
+    for (const Place& o : others)
+        if (overlap(out, o)) return true;
+    return false;
+}
+static Place scales_of(const float* scales, int rows, int columns) { return {scales, sizeof(float) * (size_t)rows * ((columns + 127) / 128)}; }
+
 static slim_status_t check_norm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, const void* H) {
     if (!X || !gamma || b < 1 || d < 1 || !(eps > 0.f) || !std::isfinite(eps)) return SLIM_ERR_INVALID_ARG;
     if (d % 16 != 0 || d > 32768) return SLIM_ERR_UNSUPPORTED_SHAPE;
-    return aligned16(X) && aligned16(residual) && aligned16(gamma) && aligned16(H) ? SLIM_OK : SLIM_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(residual) || !aligned16(gamma) || !aligned16(H)) return SLIM_ERR_INVALID_ARG;
+    // H may be X or residual (a thread has read what it writes), but no other rows of them
+    const size_t bytes = 2 * (size_t)b * d;
+    if ((H != X && overlap({H, bytes}, {X, bytes})) || (H != residual && overlap({H, bytes}, {residual, bytes})) || overlap({H, bytes}, {gamma, 2 * (size_t)d}))
+        return SLIM_ERR_INVALID_ARG;
+    return SLIM_OK;
 }
 
 slim_status_t slim_rmsnorm(const void* X, const void* residual, const void* gamma, float eps, int b, int d, void* H, void* Y, void* cuda_stream)
@@ -405,6 +427,8 @@ slim_status_t slim_rmsnorm(const void* X, const void* residual, const void* gamm
     const slim_status_t st = check_norm(X, residual, gamma, eps, b, d, H);
     if (!Y || !aligned16(Y) || Y == X || Y == residual || Y == gamma || Y == H) return SLIM_ERR_INVALID_ARG;
     if (st != SLIM_OK) return st;
+    const size_t bytes = 2 * (size_t)b * d;
+    if (overlaps_any({Y, bytes}, {{X, bytes}, {residual, bytes}, {gamma, 2 * (size_t)d}, {H, bytes}})) return SLIM_ERR_INVALID_ARG;
     return launch_rmsnorm(X, residual, gamma, eps, b, d, H, Y, 0, nullptr, nullptr, (cudaStream_t)cuda_stream);
 }
 
@@ -415,6 +439,8 @@ slim_status_t slim_rmsnorm_fp8(const void* X, const void* residual, const void* 
     const slim_status_t st = check_norm(X, residual, gamma, eps, b, d, H);
     if (!codes || !scales || !aligned16(codes) || !aligned4(scales) || !is_fp8(format)) return SLIM_ERR_INVALID_ARG;
     if (st != SLIM_OK) return st;
+    const Place c = {codes, (size_t)b * d}, s = scales_of(scales, b, d), x = {X, 2 * c.bytes}, r = {residual, 2 * c.bytes}, g = {gamma, 2 * (size_t)d}, h = {H, 2 * c.bytes};
+    if (overlaps_any(c, {x, r, g, h, s}) || overlaps_any(s, {x, r, g, h})) return SLIM_ERR_INVALID_ARG;
     return launch_rmsnorm(X, residual, gamma, eps, b, d, H, nullptr, format, codes, scales, (cudaStream_t)cuda_stream);
 }
 
@@ -424,6 +450,8 @@ slim_status_t slim_quant_fp8(const void* X, int b, int d, slim_fp8_t format, voi
     if (!X || !codes || !scales || b < 1 || d < 1 || too_long(d) || !is_fp8(format)) return SLIM_ERR_INVALID_ARG;
     if (d % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(X) || !aligned16(codes) || !aligned4(scales)) return SLIM_ERR_INVALID_ARG;
+    const Place c = {codes, (size_t)b * d}, s = scales_of(scales, b, d), x = {X, 2 * c.bytes};
+    if (overlaps_any(c, {x, s}) || overlap(s, x)) return SLIM_ERR_INVALID_ARG;
     return launch_quant_fp8(X, b, d, format, codes, scales, (cudaStream_t)cuda_stream);
 }
 
@@ -433,6 +461,8 @@ slim_status_t slim_pack_fp8(const void* W, slim_type_t type, int d_out, int d_in
     if (!W || !codes || !scales || d_out < 1 || d_in < 1 || too_long(d_out) || too_long(d_in) || !is_fp8(format) || (type != SLIM_TYPE_BF16 && type != SLIM_TYPE_F32)) return SLIM_ERR_INVALID_ARG;
     if (d_in % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(W) || !aligned16(codes) || !aligned4(scales)) return SLIM_ERR_INVALID_ARG;
+    const Place c = {codes, (size_t)d_out * d_in}, s = scales_of(scales, (d_out + 127) / 128, d_in), w = {W, (type == SLIM_TYPE_BF16 ? 2 : 4) * c.bytes};
+    if (overlaps_any(c, {w, s}) || overlap(s, w)) return SLIM_ERR_INVALID_ARG;
     return launch_pack_fp8(W, type, d_out, d_in, format, codes, scales, (cudaStream_t)cuda_stream);
 }
 
@@ -444,6 +474,7 @@ slim_status_t slim_linear_fwd_fp8(const void* Xq, const float* Xs, slim_fp8_t x_
     if (too_long(b) || too_long(d_out) || too_long(d_in)) return SLIM_ERR_INVALID_ARG;
     if (d_in % 16 != 0) return SLIM_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(Xq) || !aligned16(Wq) || !aligned16(Y) || !aligned4(Xs) || !aligned4(Ws) || !aligned4(status_dev)) return SLIM_ERR_INVALID_ARG;
+    if (Y == Xq || Y == Xs || Y == Wq || Y == Ws) return SLIM_ERR_INVALID_ARG;
     slim_status_t err;
     if (!device_info(&err)) return err;
     return launch_fp8(static_cast<const uint8_t*>(Xq), Xs, x_format, b, static_cast<const uint8_t*>(Wq), Ws, w_format, d_out, d_in,
