@@ -18,6 +18,7 @@
 //     333, 8192 -> 8192   p256 31.4, p128 37.5, r128 41.3, r64 52.4, c128 64.2, r32 94.1
 //     600, 8192 -> 8192   p128 53.8, p256 59.9, r128 60.7, r64 84.7, r32 140
 #pragma once
+#include <cmath>
 
 namespace slim {
 
@@ -42,9 +43,10 @@ inline Fp8Plan fp8_plan(int b, int d_out, int groups, int sms, int pairs, const 
     auto up = [](long long a, long long n) { return (a + n - 1) / n; };
     const long long blocks = up(d_out, 128);
     if (b <= 32) return {b <= 16 ? FP8_CLUSTER_16 : FP8_CLUSTER_32, fp8_cluster_ctas(blocks, groups, clusters[b <= 16 ? 0 : 1])};
-    auto feed = [](long long tiles, int groups, int tokens, int rows) { return (long long)((double)tiles * groups * (tokens + rows) * 128 / 11700); };
+    // (times are doubles: those of the largest sizes pass 2^63 ns)
+    auto feed = [](long long tiles, int groups, int tokens, int rows) { return std::floor((double)tiles * groups * (tokens + rows) * 128 / 11700); };
     Fp8Plan best = {FP8_PAIR_256, 1};
-    long long least = 1ll << 62;
+    double least = HUGE_VAL;
     struct Cluster { Fp8Kernel kernel; int tokens; long long alone, together, group; };      // (fixed times of one CTA and of several)
     const Cluster cuts[] = {{FP8_CLUSTER_32, 32, 2250, 3750, 360}, {FP8_CLUSTER_64, 64, 3000, 5000, 300}, {FP8_CLUSTER_128, 128, 4500, 6500, 450}};
     for (const Cluster& k : cuts) {
@@ -52,8 +54,8 @@ inline Fp8Plan fp8_plan(int b, int d_out, int groups, int sms, int pairs, const 
         const int (&resident)[4] = clusters[k.kernel - FP8_CLUSTER_16];
         const int ctas = fp8_cluster_ctas(tiles, groups, resident);
         const long long rounds = up(tiles, resident[ctas == 1 ? 0 : ctas == 2 ? 1 : ctas == 4 ? 2 : 3]);
-        const long long walk = rounds * ((ctas > 1 ? k.together : k.alone) + up(groups, ctas) * k.group), bytes = feed(tiles, groups, k.tokens, 128);
-        const long long cost = walk > bytes ? walk : bytes;
+        const double walk = (double)rounds * ((ctas > 1 ? k.together : k.alone) + up(groups, ctas) * k.group), bytes = feed(tiles, groups, k.tokens, 128);
+        const double cost = walk > bytes ? walk : bytes;
         if (cost < least && parts <= 65535) { least = cost; best = {k.kernel, ctas}; }       // (the grid has a row for each part of the tokens)
     }
     if (b <= 64) return best;
@@ -62,8 +64,8 @@ inline Fp8Plan fp8_plan(int b, int d_out, int groups, int sms, int pairs, const 
                           {FP8_PAIR_128, 256, 128, 3500, 270}, {FP8_PAIR_256, 256, 256, 4300, 420}};
     for (const Tile& k : kinds) {
         const long long n = up(b, k.tokens) * up(d_out, k.rows);
-        const long long walk = k.fixed + up(n, k.tokens == 256 ? pairs : sms) * groups * k.group, bytes = k.fixed + feed(n, groups, k.tokens, k.rows);
-        const long long cost = walk > bytes ? walk : bytes;
+        const double walk = k.fixed + (double)up(n, k.tokens == 256 ? pairs : sms) * groups * k.group, bytes = k.fixed + feed(n, groups, k.tokens, k.rows);
+        const double cost = walk > bytes ? walk : bytes;
         if (cost < least) { least = cost; best = {k.kernel, 1}; }
     }
     return best;
