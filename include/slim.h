@@ -414,13 +414,26 @@ slim_kernel_t slim_select_kernel(int b, int d_out, int d_in, int r);
 int slim_last_launch_count(void);
 
 /*
- * Token-tile width (64, 128 or 256 tokens) of the variant of the prefill kernel that the last slim_linear_fwd* call on this host
- * thread launched, 0 if that call ran another kernel.  The CTA-pair kernel cuts the tokens evenly into tiles of up to 256 (so up to 128
+ * Token-tile width of the kernel that the last slim_linear_fwd* call on this host thread launched: of the variant of the prefill kernel (64, 128
+ * or 256 tokens) or of the 8-bit layer's kernel (16 to 256; slim_last_fp8_kernel), 0 if that call ran another one.  The CTA-pair kernel cuts the tokens evenly into tiles of up to 256 (so up to 128
  * tokens are one tile of the 128 or 64 variant, however many tiles the rows make), or more finely, into tiles of up to 128 or 64, where every
  * tile then has a pair of its own and that is faster; the one-CTA kernel's width is 64.  Tests use this query to
  * make sure they exercise the variant they mean to.
  */
 int slim_last_token_tile(void);
+
+/*
+ * The 8-bit layer's kernel that the last slim_linear_fwd_fp8 on this host thread launched, SLIM_FP8_KERNEL_NONE if the last call was another one
+ * or launched nothing.  A cluster of 1, 2, 4 or 8 CTAs (*cluster_ctas, where not NULL; 1 for the others) has 128 rows of the weight and up to as many
+ * tokens as its name says; a CTA by itself has 128 tokens and as many rows as its name says, a CTA pair 256 tokens and as many.
+ */
+typedef enum {
+    SLIM_FP8_KERNEL_NONE = 0,
+    SLIM_FP8_CLUSTER_16 = 1, SLIM_FP8_CLUSTER_32 = 2, SLIM_FP8_CLUSTER_64 = 3, SLIM_FP8_CLUSTER_128 = 4,
+    SLIM_FP8_ROWS_32 = 5, SLIM_FP8_ROWS_64 = 6, SLIM_FP8_ROWS_128 = 7,
+    SLIM_FP8_PAIR_128 = 8, SLIM_FP8_PAIR_256 = 9
+} slim_fp8_kernel_t;
+slim_fp8_kernel_t slim_last_fp8_kernel(int* cluster_ctas);
 
 const char* slim_strerror(slim_status_t status);
 const char* slim_version(void);

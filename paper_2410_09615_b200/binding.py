@@ -23,6 +23,7 @@ NATIVE_PATH = os.path.join(_HERE, "_slim_native.so")
  SLIM_ERR_WORKSPACE, SLIM_ERR_CUDA, SLIM_ERR_TIMEOUT, SLIM_ERR_ARCH) = range(9)
 KERNEL_AUTO, KERNEL_SIMPLE, KERNEL_DECODE, KERNEL_PREFILL, KERNEL_PREFILL_PAIR, KERNEL_SMALL = range(6)
 KERNEL_NAMES = {KERNEL_AUTO: "auto", KERNEL_SIMPLE: "simple", KERNEL_DECODE: "decode", KERNEL_PREFILL: "prefill", KERNEL_PREFILL_PAIR: "prefill_pair", KERNEL_SMALL: "small"}
+FP8_KERNEL_NAMES = ("none", "cluster_16", "cluster_32", "cluster_64", "cluster_128", "rows_32", "rows_64", "rows_128", "pair_128", "pair_256")
 WORKSPACE_SYNC_BYTES = 256
 NOALLOC_SCRATCH_BYTES = 16 << 20
 LAYOUT_DECODE_TILED = 1
@@ -61,6 +62,7 @@ SIGNATURES = {
     "slim_decode_layout_hint": (_I, [_I, _I, _I, _I]),
     "slim_last_launch_count": (_I, []),
     "slim_last_token_tile": (_I, []),
+    "slim_last_fp8_kernel": (_I, [_P]),
     "slim_strerror": (ctypes.c_char_p, [_I]),
     "slim_version": (ctypes.c_char_p, []),
 }
@@ -189,6 +191,13 @@ def slim_last_launch_count() -> int:
 
 def slim_last_token_tile() -> int:
     return int(lib().slim_last_token_tile())
+
+
+def slim_last_fp8_kernel():
+    """(name, CTAs of a cluster) of the 8-bit layer's kernel that this thread's last slim_linear_fwd_fp8 launched; ("none", 1) behind another call."""
+    ctas = ctypes.c_int()
+    kernel = lib().slim_last_fp8_kernel(ctypes.byref(ctas))
+    return FP8_KERNEL_NAMES[kernel], ctas.value
 
 
 def new_workspace(b: int, d_out: int, d_in: int, r: int, device="cuda") -> torch.Tensor:

@@ -13,10 +13,13 @@ static std::atomic<bool> g_info_ready[64];
 static std::mutex g_info_mutex;
 static thread_local int t_launches = 0;
 static thread_local int t_token_tile = 0;
+static thread_local slim_fp8_kernel_t t_fp8_kernel = SLIM_FP8_KERNEL_NONE;
+static thread_local int t_fp8_ctas = 1;
 
 void count_launch(int n) { t_launches += n; }
-void reset_launch_count() { t_launches = 0; t_token_tile = 0; }
+void reset_launch_count() { t_launches = 0; t_token_tile = 0; t_fp8_kernel = SLIM_FP8_KERNEL_NONE; t_fp8_ctas = 1; }
 void note_token_tile(int n) { t_token_tile = n; }
+void note_fp8_kernel(slim_fp8_kernel_t kernel, int ctas) { t_fp8_kernel = kernel; t_fp8_ctas = ctas; }
 
 // The record of a device is filled once under the mutex and published with a release store;
 // readers take it with an acquire load, so they never see a half-written record.
@@ -484,6 +487,12 @@ slim_status_t slim_linear_fwd_fp8(const void* Xq, const float* Xs, slim_fp8_t x_
 int slim_last_launch_count(void) { return t_launches; }
 
 int slim_last_token_tile(void) { return t_token_tile; }
+
+slim_fp8_kernel_t slim_last_fp8_kernel(int* cluster_ctas)
+{
+    if (cluster_ctas) *cluster_ctas = t_fp8_ctas;
+    return t_fp8_kernel;
+}
 
 const char* slim_strerror(slim_status_t status)
 {

@@ -94,7 +94,8 @@ __device__ __forceinline__ float bf16_tail(float v) {
 // Launch bookkeeping for slim_last_launch_count().
 void count_launch(int n);
 void reset_launch_count();
-void note_token_tile(int n);      // token-tile width of the prefill main launch, for slim_last_token_tile()
+void note_token_tile(int n);      // token-tile width of the prefill main launch or the 8-bit layer's, for slim_last_token_tile()
+void note_fp8_kernel(slim_fp8_kernel_t kernel, int ctas);         // for slim_last_fp8_kernel()
 
 // ---- launchers (defined in the kernel files) --------------------------------
 slim_status_t launch_pack(const int8_t* codes, const uint8_t* mask, int d_out, int d_in,

@@ -890,18 +890,24 @@ slim_status_t launch_fp8(const uint8_t* Xq, const float* Xs, int x_format, int b
     Fp8Params p = {};
     p.Y = Y; p.Xs = Xs; p.Ws = Ws; p.status = status_dev; p.b = b; p.d_out = d_out; p.groups = ceil_div(d_in, kF8Group);
     const Fp8Plan plan = fp8_plan(b, d_out, p.groups, di->sm_count, dev->pairs, dev->clusters);
-    switch (plan.kernel) {
-    case FP8_CLUSTER_16:  return launch_small8<16>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
-    case FP8_CLUSTER_32:  return launch_small8<32>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
-    case FP8_CLUSTER_64:  return launch_small8<64>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
-    case FP8_CLUSTER_128: return launch_small8<128>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
-    case FP8_ROWS_32:     return launch_tokens8<32, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
-    case FP8_ROWS_64:     return launch_tokens8<64, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
-    case FP8_ROWS_128:    return launch_tokens8<128, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
-    case FP8_PAIR_128:    return launch_tokens8<128, true>(p, Xq, x_format, Wq, w_format, d_in, dev->pairs, st);
-    case FP8_PAIR_256:    return launch_tokens8<256, true>(p, Xq, x_format, Wq, w_format, d_in, dev->pairs, st);
-    }
-    return SLIM_ERR_UNSUPPORTED_SHAPE;
+    auto launch = [&]() -> slim_status_t {
+        switch (plan.kernel) {
+        case FP8_CLUSTER_16:  return launch_small8<16>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
+        case FP8_CLUSTER_32:  return launch_small8<32>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
+        case FP8_CLUSTER_64:  return launch_small8<64>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
+        case FP8_CLUSTER_128: return launch_small8<128>(p, Xq, x_format, Wq, w_format, d_in, plan.ctas, di->sm_count, st);
+        case FP8_ROWS_32:     return launch_tokens8<32, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
+        case FP8_ROWS_64:     return launch_tokens8<64, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
+        case FP8_ROWS_128:    return launch_tokens8<128, false>(p, Xq, x_format, Wq, w_format, d_in, di->sm_count, st);
+        case FP8_PAIR_128:    return launch_tokens8<128, true>(p, Xq, x_format, Wq, w_format, d_in, dev->pairs, st);
+        case FP8_PAIR_256:    return launch_tokens8<256, true>(p, Xq, x_format, Wq, w_format, d_in, dev->pairs, st);
+        }
+        return SLIM_ERR_UNSUPPORTED_SHAPE;
+    };
+    err = launch();
+    static_assert(SLIM_FP8_CLUSTER_16 == 1 + (int)FP8_CLUSTER_16 && SLIM_FP8_PAIR_256 == 1 + (int)FP8_PAIR_256, "the plan's kernels in the header's order");
+    if (err == SLIM_OK) note_fp8_kernel(static_cast<slim_fp8_kernel_t>(1 + (int)plan.kernel), plan.ctas);
+    return err;
 }
 
 }  // namespace slim
