@@ -55,7 +55,7 @@ __device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint32_t a_lo, uint
 // A warp's bounded wait (tcgen05.cuh's mbar_wait, for lanes that go on together: the vote tells the compiler so, and spares it bringing them
 // together again before every instruction of a whole warp).  One that expires raises the CTA's flag, which ends all others and is looked
 // at at the end.  False: it gave up; a loader then asks for no more.  (The issuing warp does not look: its MMAs go on over what the stages hold, one
-// group in the time that such a wait takes, and a branch on the answer took 100 tokens, 8192 -> 8192 from 20.1 us to 22.5.)
+// group in the time that such a wait takes, and a branch on the answer took 100 tokens, 8192 -> 8192 from 20.1 us to 21.8.)
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* abort_flag) {
     for (uint32_t it = 0; it < kPSpinLimit; ++it) {
         if (__all_sync(0xffffffffu, mbar_try(bar, parity, false))) return true;
@@ -178,7 +178,7 @@ __device__ __forceinline__ uint32_t peer(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// Rows r, r + 8 of tokens c, c + 1 (see the file's header) into Y.  Lanes four apart have neighbouring rows: they swap, and each stores two
+// Rows r, r + 8 of tokens c, c + 1 (what tcgen05.ld 16x256b gives a lane: above fp8_small_kernel) into Y.  Lanes four apart have neighbouring rows: they swap, and each stores two
 // rows of one token at once where rows of Y are a whole number of words.
 __device__ __forceinline__ void store_frag(__nv_bfloat16* Y, int d_out, int row, int token, int b, float2 lo, float2 hi, int lane) {
     const bool odd = lane & 4;
@@ -526,7 +526,7 @@ fp8_tokens_kernel(const Fp8TokensParams p, const __grid_constant__ CUtensorMap t
     uint64_t* acc_full = empty + kStages;            // [kBuffers] a group's MMAs are complete
     uint64_t* acc_empty = acc_full + kBuffers;       // [kBuffers] even CTA: the warps of both CTAs have read the buffer
     uint64_t* sc_full = acc_empty + kBuffers;        // [kSlots] the scales of eight groups are there
-    uint64_t* sc_empty = sc_full + kSlots;           // [kSlots] eight warps have read them
+    uint64_t* sc_empty = sc_full + kSlots;           // [kSlots] the accumulating warps have read them
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sc_empty + kSlots);
     volatile uint32_t* abort_flag = tmem_slot + 1;
 

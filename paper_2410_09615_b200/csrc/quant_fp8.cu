@@ -1,8 +1,11 @@
 // What feeds a linear layer: the residual's addition and the root-mean-square norm, with a bf16 or an 8-bit output, and the
 // quantisers that make 8-bit operands of activations (groups of 128 columns of a row) and of weights (blocks of 128 x 128).
-// Definitions: include/slim.h.  All of them read every input once and write every output once; the HBM bounds them (share of a copy's
+// Definitions: include/slim.h.  All of them read every input once and write every output once.  The HBM bounds most of them (share of a copy's
 // 6456 GB/s, inputs in rotation: norm of 4096 x 8192 with residual into 8 bits 37.4 us, 97 %; 2048 x 13824 into 8 bits 14.0 us, 94 %;
-// a weight of 11008 x 4096 20.9 us, 100 %), or, for few rows, a launch and a trip to it (1.3 to 2.1 us).
+// a bf16 weight of 11008 x 4096 20.9 us, 100 %), or, for few rows, a launch and a trip to it (1.3 to 2.1 us).  Two forms do not reach it, since few
+// CTAs fit on an SM and each loads all it has before it stores: a weight from binary32 (96 registers, two CTAs: 4096 x 4096 17.6 us, 74 %; 11008 x 4096
+// 44.4 us, 79 %; 8192 x 28672 209 us, 87 %) and norms of more than 16384 columns (1024 threads of 50 registers, one CTA: 300 x 28672 with residual into
+// 8 bits 18.0 us, 52 %; 2000 x 28672 82.5 us, 75 %).
 #include "fp8.cuh"
 
 namespace slim {
