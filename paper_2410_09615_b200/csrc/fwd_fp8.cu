@@ -178,8 +178,8 @@ __device__ __forceinline__ uint32_t peer(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// Rows r, r + 8 of tokens c, c + 1 (what tcgen05.ld 16x256b gives a lane: above fp8_small_kernel) into Y.  Lanes four apart have neighbouring rows: they swap, and each stores two
-// rows of one token at once where rows of Y are a whole number of words.
+// Rows r, r + 8 of tokens c, c + 1 (what tcgen05.ld 16x256b gives a lane: above fp8_small_kernel) into Y.  Lanes four apart have neighbouring
+// rows: they swap, and each stores two rows of one token at once where rows of Y are a whole number of words.
 __device__ __forceinline__ void store_frag(__nv_bfloat16* Y, int d_out, int row, int token, int b, float2 lo, float2 hi, int lane) {
     const bool odd = lane & 4;
     const float give_lo = odd ? lo.x : lo.y, give_hi = odd ? hi.x : hi.y;
